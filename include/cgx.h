@@ -89,7 +89,8 @@ typedef enum {
 
 typedef enum {
     CGX_F32 = 0,           /* gradient stored as IEEE binary32 */
-    CGX_F16 = 1            /* gradient stored as IEEE binary16, arithmetic in binary32 */
+    CGX_F16 = 1,           /* gradient stored as IEEE binary16, arithmetic in binary32 */
+    CGX_BF16 = 2           /* bfloat16: the cgx_head_* and cgx_grad_* calls only (CGX_ERR_DTYPE elsewhere) */
 } cgx_dtype;
 
 #define CGX_MAX_PEERS 64
@@ -390,6 +391,77 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
                                  const uint8_t *width_candidates /* host [k] */, int32_t k,
                                  const int32_t *bucket_candidates /* host [kb] */, int32_t kb,
                                  int32_t *buckets_out /* host [L] */);
+
+/*
+ * What stands in front of the fused buffer in a language model's training step: the loss over the
+ * vocabulary, whose weight is the largest layer of every Transformer plan, and the clipping of all
+ * gradients by their global norm.  These calls take no plan; they allocate nothing, copy nothing from
+ * the host on the stream, and may be captured into a graph.
+ *
+ * Softmax cross entropy of a head (the last matrix product of a language model) without its logits.
+ *   z[n][v] = sum_h hidden[n][h] * weight[v][h]
+ *   lse[n]  = log(sum_v exp(z[n][v])),  loss[n] = lse[n] - z[n][targets[n]]
+ * cgx_head_loss writes loss and lse.  Given that lse and one factor per token (dloss: the derivative of
+ * what the step minimises by loss[n]; 1 / tokens for a mean), cgx_head_loss_grad writes
+ *   d[n][v]       = dloss[n] * (exp(z[n][v] - lse[n]) - (v == targets[n]))
+ *   dhidden[n][h] = sum_v d[n][v] * weight[v][h],  dweight[v][h] = sum_n d[n][v] * hidden[n][h]
+ * Logits are formed tile by tile and kept by neither call; the second one forms them again, holds d for a
+ * piece of the vocabulary at a time in the workspace, and in the type of the operands (for binary16 under
+ * a power of two that keeps it in range).  Products are summed in binary32, each result is rounded once.
+ * The order of every sum is fixed: the same call gives the same bits again.
+ *   hidden    device, tokens x width elements of dt (CGX_F32, CGX_F16 or CGX_BF16), dense
+ *   weight    device, vocab x width elements of dt, dense
+ *   targets   device, tokens int64 (8-byte aligned).  A token whose target is `ignore` has loss and lse 0
+ *             and a dhidden row of zeros, and takes no part in dweight, whatever its hidden state holds
+ *             (NaN and infinities too); so has, in cgx_head_loss_grad, one whose dloss is 0.  Any other target
+ *             outside [0, vocab) makes that token's loss and gradients NaN.
+ *   loss, lse, dloss   device, tokens floats (4-byte aligned)
+ *   dhidden, dweight   device, tokens x width and vocab x width elements of dt; every element is written
+ *   workspace device, 16-byte aligned, at least the bytes cgx_head_workspace reports (CGX_ERR_SIZE
+ *             otherwise); contents unspecified before and after.  Calls that share one must not overlap.
+ * tokens may be 0 (dweight is then zero); 1 <= width <= 2^17, 1 <= vocab < 2^31, tokens < 2^24.
+ */
+int cgx_head_workspace(int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt,
+                       int32_t grad /* 0: for cgx_head_loss; else for both calls */, size_t *bytes);
+int cgx_head_loss(const void *hidden, const void *weight, const int64_t *targets, int64_t tokens, int32_t width,
+                  int64_t vocab, cgx_dtype dt, int64_t ignore, float *loss, float *lse, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *targets, const float *lse,
+                       const float *dloss, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt,
+                       int64_t ignore, void *dhidden, void *dweight, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/*
+ * Global l2 norm of a list of gradient tensors, and their clipping by it.
+ *   norm   = sqrt(sum over all tensors and elements of x^2), summed in binary64 in a fixed order, rounded to
+ *            binary32 at the end
+ *   factor = max_norm / norm where norm > max_norm, else 1 (binary32); a NaN norm gives a NaN factor
+ *   x * factor in binary32, rounded once to the type it is stored in
+ * cgx_grad_norm writes norm.  cgx_grad_clip reads norm (its own call's, or one that also covers other ranks'
+ * tensors) and scales the tensors in place (out = NULL; nothing is written where the factor is 1), or writes
+ * them one after another, in list order, into `out`: the fused buffer that cgx_quantize takes, in its type.
+ *   tensors    host, count entries; read during the call.  Every tensor is dense, aligned like its
+ *              elements, and may have any length, 0 included.  Tensors must not overlap where they are
+ *              scaled in place.
+ *   norm       device, one float (4-byte aligned)
+ *   out        device, 16-byte aligned, as many elements of out_dt as the tensors have together; overlaps none
+ *              of them
+ *   workspace  device, 16-byte aligned, at least the bytes cgx_grad_norm_workspace reports (CGX_ERR_SIZE
+ *              otherwise).  Calls that share one must not overlap.
+ * A launch covers up to 160 tensors; longer lists take more.
+ */
+typedef struct {
+    void *data;       /* device */
+    int64_t n;        /* elements */
+    int32_t dt;       /* cgx_dtype */
+    int32_t reserved; /* 0 */
+} cgx_tensor;
+
+int cgx_grad_norm_workspace(size_t *bytes);
+int cgx_grad_norm(const cgx_tensor *tensors, int32_t count, float *norm, void *workspace, size_t workspace_bytes,
+                  void *stream);
+int cgx_grad_clip(const cgx_tensor *tensors, int32_t count, const float *norm, float max_norm, void *out,
+                  cgx_dtype out_dt, void *stream);
 
 /* Human-readable name of a status code (static storage). */
 const char *cgx_status_string(int status);

@@ -18,7 +18,7 @@ import numpy as np
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcgx.so")
 
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2         # BF16: the cgx_head_* and cgx_grad_* calls
 MAX_PEERS = 64
 MAX_FUSED_PEERS = 16
 
@@ -32,7 +32,8 @@ EXPORTS = ("cgx_sizes", "cgx_quantize", "cgx_dequant_reduce", "cgx_dequant_reduc
            "cgx_layered_stats_workspace", "cgx_layered_layer_sqerrors", "cgx_qsgd_layered_sizes",
            "cgx_qsgd_layered_quantize", "cgx_qsgd_layered_dequant_reduce", "cgx_qsgd_layered_dequant_reduce_requantize",
            "cgx_plan_tiles", "cgx_plan_tiles_chunk", "cgx_stream_probe", "cgx_stream_probe_shaped",
-           "cgx_issue_probe", "cgx_issue_probe_form", "cgx_status_string", "cgx_shutdown")
+           "cgx_issue_probe", "cgx_issue_probe_form", "cgx_head_workspace", "cgx_head_loss", "cgx_head_loss_grad",
+           "cgx_grad_norm_workspace", "cgx_grad_norm", "cgx_grad_clip", "cgx_status_string", "cgx_shutdown")
 
 TILE_DTYPE = np.dtype([("elem0", "<i8"), ("packed_off", "<i8"), ("bucket0", "<u4"), ("count", "<u4"),
                        ("info", "<u4"), ("pad", "<u4")])
@@ -110,6 +111,14 @@ def lib() -> ctypes.CDLL:
         L.cgx_issue_probe.argtypes = [c.c_int32, c.c_int32, c.c_int32, c.c_void_p, c.c_size_t, c.c_void_p]
         L.cgx_issue_probe_form.restype = c.c_char_p
         L.cgx_issue_probe_form.argtypes = [c.c_int32]
+        L.cgx_head_workspace.argtypes = [c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int32, c.POINTER(c.c_size_t)]
+        L.cgx_head_loss.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int64,
+                                    c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.cgx_head_loss_grad.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64,
+                                         c.c_int, c.c_int64, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.cgx_grad_norm_workspace.argtypes = [c.POINTER(c.c_size_t)]
+        L.cgx_grad_norm.argtypes = [c.c_void_p, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.cgx_grad_clip.argtypes = [c.c_void_p, c.c_int32, c.c_void_p, c.c_float, c.c_void_p, c.c_int, c.c_void_p]
         L.cgx_status_string.restype = c.c_char_p
         L.cgx_status_string.argtypes = [c.c_int]
         L.cgx_shutdown.argtypes = []
@@ -133,6 +142,10 @@ class _PythonChecks:
 
     @staticmethod
     def tables(packed, meta, packed_bytes, meta_bytes):
+        return None
+
+    @staticmethod
+    def gradients(tensors):
         return None
 
     @staticmethod
@@ -255,7 +268,7 @@ def _stream(stream) -> int:
 
 _TORCH_DTYPES = {F32: "float32", F16: "float16"}
 #: element types by the numbers the extension module knows
-_TYPE_CODES = {None: 0, "float32": 1, "float16": 2, "float64": 3}
+_TYPE_CODES = {None: 0, "float32": 1, "float16": 2, "float64": 3, "bfloat16": 4, "int64": 5}
 
 
 _dtype_objects = {}
@@ -614,6 +627,117 @@ def cgx_stream_probe(src, read_bytes: int, dst, write_bytes: int, stream=None) -
     _check(lib().cgx_stream_probe(_device_buffer(src, "cgx_stream_probe: src", read_bytes), read_bytes,
                                   _device_buffer(dst, "cgx_stream_probe: dst", write_bytes), write_bytes,
                                   _stream(stream)), "cgx_stream_probe")
+
+
+_HEAD_TYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}
+_TORCH_NAMES = {F32: "float32", F16: "float16", BF16: "bfloat16"}
+
+
+def cgx_head_workspace(tokens: int, width: int, vocab: int, dt: int, grad: bool = False) -> int:
+    """Bytes of device workspace cgx_head_loss needs; with grad, cgx_head_loss_grad as well."""
+    nbytes = ctypes.c_size_t()
+    _check(lib().cgx_head_workspace(tokens, width, vocab, dt, int(bool(grad)), ctypes.byref(nbytes)), "cgx_head_workspace")
+    return int(nbytes.value)
+
+
+def _head(name: str, hidden, weight, targets):
+    """(tokens, width, vocab, dt, addresses of hidden, weight, targets) of a head's call."""
+    for t, what in ((hidden, "hidden"), (weight, "weight")):
+        if getattr(t, "ndim", 0) != 2:
+            raise ValueError(f"{name}: {what}: a matrix is needed, a row for each {'token' if what == 'hidden' else 'entry of the vocabulary'}")
+    (tokens, width), (vocab, across) = hidden.shape, weight.shape
+    dt = _HEAD_TYPES.get(str(hidden.dtype))
+    if dt is None:
+        raise ValueError(f"{name}: hidden: element type {hidden.dtype}, expected torch.float32, torch.float16 or torch.bfloat16")
+    if across != width:
+        raise ValueError(f"{name}: weight: rows of {across} elements, those of hidden have {width}")
+    if targets.numel() != tokens:
+        raise ValueError(f"{name}: targets: {targets.numel()} entries for {tokens} tokens")
+    size = 4 if dt == F32 else 2
+    return (tokens, width, vocab, dt, _device_buffer(hidden, (name, "hidden"), tokens * width * size, _TORCH_NAMES[dt]),
+            _device_buffer(weight, (name, "weight"), vocab * width * size, _TORCH_NAMES[dt]),
+            _device_buffer(targets, (name, "targets"), tokens * 8, "int64"))
+
+
+def cgx_head_loss(hidden, weight, targets, loss, lse, workspace, ignore: int = -100, stream=None) -> None:
+    """Softmax cross entropy of the head hidden @ weight.T without its logits: loss and lse (device float32[tokens]) of every token.
+    hidden: [tokens, width] and weight: [vocab, width] of one type (float32, float16, bfloat16); targets: int64[tokens], `ignore`
+    marks tokens without one (loss and lse 0); workspace: device tensor of cgx_head_workspace bytes."""
+    name = "cgx_head_loss"
+    tokens, width, vocab, dt, h, w, t = _head(name, hidden, weight, targets)
+    out, sums = (_device_buffer(x, (name, what), tokens * 4, "float32") for x, what in ((loss, "loss"), (lse, "lse")))
+    ws = _device_buffer(workspace, (name, "workspace"), 0)              # its size travels with the call: the library checks it
+    _check(lib().cgx_head_loss(h, w, t, tokens, width, vocab, dt, ignore, out, sums, ws, workspace.numel() * workspace.element_size(),
+                               _stream(stream)), name)
+
+
+def cgx_head_loss_grad(hidden, weight, targets, lse, dloss, dhidden, dweight, workspace, ignore: int = -100, stream=None) -> None:
+    """Gradients of sum(dloss * loss) by hidden and weight, into dhidden and dweight (their shapes and type).  lse: from
+    cgx_head_loss of the same hidden, weight and targets; dloss: device float32[tokens], 0 for tokens that take no part;
+    workspace: device tensor of cgx_head_workspace(..., grad=True) bytes."""
+    name = "cgx_head_loss_grad"
+    tokens, width, vocab, dt, h, w, t = _head(name, hidden, weight, targets)
+    size = 4 if dt == F32 else 2
+    sums, factors = (_device_buffer(x, (name, what), tokens * 4, "float32") for x, what in ((lse, "lse"), (dloss, "dloss")))
+    dh = _device_buffer(dhidden, (name, "dhidden"), tokens * width * size, _TORCH_NAMES[dt])
+    dw = _device_buffer(dweight, (name, "dweight"), vocab * width * size, _TORCH_NAMES[dt])
+    ws = _device_buffer(workspace, (name, "workspace"), 0)
+    _check(lib().cgx_head_loss_grad(h, w, t, sums, factors, tokens, width, vocab, dt, ignore, dh, dw, ws,
+                                    workspace.numel() * workspace.element_size(), _stream(stream)), name)
+
+
+def cgx_grad_norm_workspace() -> int:
+    """Bytes of device workspace cgx_grad_norm needs."""
+    nbytes = ctypes.c_size_t()
+    _check(lib().cgx_grad_norm_workspace(ctypes.byref(nbytes)), "cgx_grad_norm_workspace")
+    return int(nbytes.value)
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dt", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def _gradients(name: str, grads: Sequence):
+    """(array of cgx_tensor, tensors, elements in all) of a list of device tensors."""
+    table = (_native or _args()).gradients(grads)
+    if table is not None:
+        return table[0], len(grads), table[1]
+    entries, total = (_Tensor * max(len(grads), 1))(), 0
+    for k, g in enumerate(grads):
+        dt = _HEAD_TYPES.get(str(getattr(g, "dtype", None)))
+        if dt is None:
+            raise ValueError(f"{name}: tensor {k}: element type {getattr(g, 'dtype', type(g).__name__)}, expected torch.float32, "
+                             "torch.float16 or torch.bfloat16")
+        entries[k] = _Tensor(_device_buffer(g, (name, "tensor", k), 0, _TORCH_NAMES[dt]), g.numel(), dt, 0)
+        total += g.numel()
+    return entries, len(grads), total
+
+
+def cgx_grad_norm(grads: Sequence, norm, workspace, stream=None) -> None:
+    """norm (device float32[1]) = l2 norm over all elements of a list of device tensors (float32, float16, bfloat16, mixed);
+    workspace: device tensor of cgx_grad_norm_workspace bytes."""
+    entries, count, _ = _gradients("cgx_grad_norm", grads)
+    out = _device_buffer(norm, "cgx_grad_norm: norm", 4, "float32")
+    ws = _device_buffer(workspace, "cgx_grad_norm: workspace", 0)
+    _check(lib().cgx_grad_norm(entries, count, out, ws, workspace.numel() * workspace.element_size(), _stream(stream)), "cgx_grad_norm")
+
+
+def cgx_grad_clip(grads: Sequence, norm, max_norm: float, out=None, stream=None) -> None:
+    """Scales the tensors by min(1, max_norm / norm): in place, or one after another into `out` (the fused buffer, float32, float16 or
+    bfloat16, as many elements as the tensors have together or more).  norm: device float32[1], from cgx_grad_norm."""
+    name = "cgx_grad_clip"
+    entries, count, total = _gradients(name, grads)
+    size = _device_buffer(norm, (name, "norm"), 4, "float32")
+    fused, dt = 0, F32
+    if out is not None:
+        dt = _HEAD_TYPES.get(str(getattr(out, "dtype", None)))
+        if dt is None:
+            raise ValueError(f"{name}: out: element type {getattr(out, 'dtype', type(out).__name__)}, expected torch.float32, "
+                             "torch.float16 or torch.bfloat16")
+        fused = _device_buffer(out, (name, "out"), total * (4 if dt == F32 else 2), _TORCH_NAMES[dt])
+        if not fused:
+            return                                                       # an empty buffer: every tensor is empty
+    _check(lib().cgx_grad_clip(entries, count, size, max_norm, fused, dt, _stream(stream)), name)
 
 
 LOAD_POLICIES = ("plain", "nt", "sc1", "sc0 sc1")

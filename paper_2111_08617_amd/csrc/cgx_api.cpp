@@ -1014,7 +1014,7 @@ const char *cgx_status_string(int status)
     switch (status) {
     case CGX_OK: return "ok";
     case CGX_ERR_NULL: return "a required pointer is NULL";
-    case CGX_ERR_SIZE: return "n or L is negative, too large, or n does not match layer_offsets[L]";
+    case CGX_ERR_SIZE: return "a size is negative, too large or too small, or n does not match layer_offsets[L]";
     case CGX_ERR_OFFSETS: return "layer_offsets must start at 0 and never decrease";
     case CGX_ERR_BITS: return "bits_per_layer entries must be 0 (pass-through) or 1..8 (2..8 for the cgx_qsgd_ calls)";
     case CGX_ERR_BUCKET: return "bucket must be a multiple of 32 in [32, 8192]";

@@ -11,7 +11,7 @@
 
 namespace {
 
-// Element types by the numbers the binding passes: any, float32, float16, float64.
+// Element types by the numbers the binding passes: any, float32, float16, float64, bfloat16, int64.
 bool type_matches(c10::ScalarType type, long code)
 {
     switch (code) {
@@ -19,6 +19,8 @@ bool type_matches(c10::ScalarType type, long code)
     case 1: return type == c10::ScalarType::Float;
     case 2: return type == c10::ScalarType::Half;
     case 3: return type == c10::ScalarType::Double;
+    case 4: return type == c10::ScalarType::BFloat16;
+    case 5: return type == c10::ScalarType::Long;
     default: return false;
     }
 }
@@ -78,6 +80,41 @@ PyObject *tables(PyObject *, PyObject *const *args, Py_ssize_t n)
     return Py_BuildValue("(y#y#)", reinterpret_cast<const char *>(packed), bytes, reinterpret_cast<const char *>(meta), bytes);
 }
 
+// A cgx_tensor of the C ABI (include/cgx.h).
+struct Entry {
+    void *data;
+    int64_t n;
+    int32_t dt, reserved;
+};
+
+// gradients(tensors) -> (a C array of cgx_tensor as bytes, elements in all), or None where one of them is no plain dense device
+// tensor of a gradient's type
+PyObject *gradients(PyObject *, PyObject *list)
+{
+    if (!(PyList_Check(list) || PyTuple_Check(list))) Py_RETURN_NONE;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(list);
+    PyObject *out = PyBytes_FromStringAndSize(nullptr, count * Py_ssize_t(sizeof(Entry)));
+    if (!out) return nullptr;
+    Entry *entries = reinterpret_cast<Entry *>(PyBytes_AS_STRING(out));
+    long long total = 0;
+    for (Py_ssize_t i = 0; i < count; i++) {
+        PyObject *obj = PySequence_Fast_GET_ITEM(list, i);
+        Entry e{nullptr, 0, -1, 0};
+        if (address_of(obj, 0, 0, &e.data)) {
+            const at::Tensor &t = THPVariable_Unpack(obj);
+            e.n = t.numel();
+            e.dt = type_matches(t.scalar_type(), 1) ? 0 : type_matches(t.scalar_type(), 2) ? 1 : type_matches(t.scalar_type(), 4) ? 2 : -1;
+        }
+        if (e.dt < 0) {
+            Py_DECREF(out);
+            Py_RETURN_NONE;
+        }
+        std::memcpy(entries + i, &e, sizeof e);
+        total += e.n;
+    }
+    return Py_BuildValue("(NL)", out, total);
+}
+
 // unchanged((address, bytes, address, bytes, ...)) -> whether the memory at every address still holds the bytes beside it
 PyObject *unchanged(PyObject *, PyObject *pairs)
 {
@@ -102,6 +139,7 @@ PyObject *unchanged(PyObject *, PyObject *pairs)
 PyMethodDef methods[] = {
     {"address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(address)), METH_FASTCALL, nullptr},
     {"tables", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tables)), METH_FASTCALL, nullptr},
+    {"gradients", gradients, METH_O, nullptr},
     {"unchanged", unchanged, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
