@@ -150,6 +150,8 @@ struct Hidden {
 
 // ---------------------------------------------------------------- logits
 
+__device__ __forceinline__ uint32_t up(int64_t v, int to) { return uint32_t((v + to - 1) / to); }
+
 template <typename K>
 using Lds = unsigned char[K::kLds];
 
@@ -163,15 +165,15 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
     using T = typename K::T;
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
-    int64_t tm, tn;
-    if (!tile_of_block(blockIdx.x, (count + K::BM - 1) / K::BM, (columns + K::BN - 1) / K::BN, tm, tn)) return;
-    const int64_t m0 = tm * K::BM, n0 = tn * K::BN;
+    int tm, tn;
+    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
+    const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     K tile;
     typename K::A a;
     typename K::B b;
     a.start(hidden.of(count), pitch, m0, count - m0, 0, int(threadIdx.x));
     b.start(weight, pitch, n0, columns - n0, 0, int(threadIdx.x));
-    tile.run(a, b, pitch / K::kDepth, K::kDepth, lds);
+    tile.run(a, b, int(pitch / K::kDepth), K::kDepth, lds);
 
     __syncthreads();
     float2 *joined = reinterpret_cast<float2 *>(lds);        // [WN][BM]
@@ -277,15 +279,15 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
-    int64_t tm, tn;
-    if (!tile_of_block(blockIdx.x, (count + K::BM - 1) / K::BM, (columns + K::BN - 1) / K::BN, tm, tn)) return;
-    const int64_t m0 = tm * K::BM, n0 = tn * K::BN;
+    int tm, tn;
+    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
+    const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     K tile;
     typename K::A a;
     typename K::B b;
     a.start(hidden.of(count), pitch, m0, count - m0, 0, int(threadIdx.x));
     b.start(weight, pitch, n0, columns - n0, 0, int(threadIdx.x));
-    tile.run(a, b, pitch / K::kDepth, K::kDepth, lds);
+    tile.run(a, b, int(pitch / K::kDepth), K::kDepth, lds);
 
     const int g = tile.lane >> 4, r = tile.lane & 15;
     const int64_t c0 = n0 + tile.wn + 4 * g;
@@ -318,16 +320,16 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
 {
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
-    int64_t tm, tn;
-    if (!tile_of_block(blockIdx.x, (count + K::BM - 1) / K::BM, (pitch + K::BN - 1) / K::BN, tm, tn)) return;
-    const int64_t m0 = tm * K::BM, n0 = tn * K::BN;
+    int tm, tn;
+    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(pitch, K::BN), tm, tn)) return;
+    const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     K tile;
     typename K::A a;
     typename K::B b;
     a.start(delta, piece, m0, count - m0, 0, int(threadIdx.x));
     b.start(weight, pitch, n0, pitch - n0, 0, int(threadIdx.x));
-    const int64_t steps = (columns + K::kDepth - 1) / K::kDepth;
-    tile.run(a, b, steps, int(columns - (steps - 1) * K::kDepth), lds);
+    const int steps = int(up(columns, K::kDepth));
+    tile.run(a, b, steps, int(columns - int64_t(steps - 1) * K::kDepth), lds);
     const int g = tile.lane >> 4, r = tile.lane & 15;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
@@ -353,16 +355,16 @@ __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *hea
     typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
-    int64_t tm, tn;
-    if (!tile_of_block(blockIdx.x, (columns + K::BM - 1) / K::BM, (width + K::BN - 1) / K::BN, tm, tn)) return;
-    const int64_t m0 = tm * K::BM, n0 = tn * K::BN;
+    int tm, tn;
+    if (!tile_of_block(blockIdx.x, up(columns, K::BM), up(width, K::BN), tm, tn)) return;
+    const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     const float unscale = header->unscale;
     K tile;
     typename K::A a;
     typename K::B b;
     a.start(delta, piece, m0, piece - m0, 0, int(threadIdx.x));
     b.start(hidden.of(count), pitch, n0, pitch - n0, 0, int(threadIdx.x));
-    tile.run(a, b, (count + K::kDepth - 1) / K::kDepth, K::kDepth, lds);
+    tile.run(a, b, int(up(count, K::kDepth)), K::kDepth, lds);
     const int g = tile.lane >> 4, r = tile.lane & 15;
     const bool fours = width % 4 == 0;
 #pragma unroll

@@ -26,16 +26,19 @@ struct Element;
 template <>
 struct Element<__bf16> {
     using Frag = bf16x8;
+    static constexpr int kProducts = 1;
     static __device__ __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Element<_Float16> {
     using Frag = f16x8;
+    static constexpr int kProducts = 1;
     static __device__ __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Element<float> {
     using Frag = f32x4;
+    static constexpr int kProducts = 4;
     static __device__ __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c)
     {
 #pragma unroll
@@ -50,10 +53,16 @@ enum Layout {
     kRowContiguous       // element (row, k) at k * pitch + row
 };
 
-__device__ __forceinline__ void to_lds(const void *src, void *dst)
+// 16 bytes per lane from base + offset (base uniform) to LDS, lane l's at address dst + 16 l (dst uniform).  Written out because the compiler,
+// which cannot tell apart the stage that such a load fills and the one that a transposing LDS read takes, makes every such read wait for all
+// loads that the builtin has issued; the waits that are needed are in Tile.
+__device__ __forceinline__ void to_lds(const void *base, uint32_t offset, uint32_t dst)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                     (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
 }
 
 // One side (ROWS rows) of a tile in LDS, kStepBytes of the summed axis deep, filled straight from memory by THREADS threads.
@@ -67,6 +76,7 @@ struct Side {
     static constexpr int kLoads = kPieces / THREADS;
     static constexpr int kBytes = ROWS * kStepBytes;
     static_assert(kPieces % THREADS == 0 && ROWS % kMnUnit == 0, "a tile side is filled by whole instructions");
+    static constexpr int kReadsPerFragment = LAYOUT == kSumContiguous ? 1 : sizeof(T) == 2 ? 2 : 4;
     static constexpr int kPiecesPerRow = LAYOUT == kSumContiguous ? kStepBytes / 16 : ROWS / kPer;
 
     const T *base;            // of the current step, uniform
@@ -116,11 +126,11 @@ struct Side {
             }
         }
     }
-    __device__ __forceinline__ void load(unsigned char *lds, int wave)
+    __device__ __forceinline__ void load(uint32_t lds, int wave)
     {
         const unsigned char *b = reinterpret_cast<const unsigned char *>(base);
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) to_lds(b + offset[i], lds + (i * THREADS + wave * 64) * 16);
+        for (int i = 0; i < kLoads; i++) to_lds(b, offset[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
         base += step;
     }
     // The fragment of rows row0 .. row0 + 15 (row0 a multiple of 16) and the half-th 64 bytes of the step.
@@ -168,25 +178,69 @@ struct Tile {
     f32x4 acc[TM][TN];
     int wave, lane, wm, wn;
 
-    __device__ __forceinline__ void multiply(const unsigned char *stage)
+    using Frag = typename Element<T>::Frag;
+    struct Frags {
+        Frag a[TM], b[TN];
+    };
+    __device__ __forceinline__ void fetch(Frags &f, const unsigned char *stage, int half) const
     {
-        using Frag = typename Element<T>::Frag;
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            Frag a[TM], b[TN];
+        for (int j = 0; j < TN; j++) f.b[j] = B::fragment(stage + A::kBytes, wn + 16 * j, half, lane);
 #pragma unroll
-            for (int j = 0; j < TN; j++) b[j] = B::fragment(stage + A::kBytes, wn + 16 * j, half, lane);
+        for (int i = 0; i < TM; i++) f.a[i] = A::fragment(stage, wm + 16 * i, half, lane);
+    }
+    __device__ __forceinline__ void multiply(const Frags &f)
+    {
 #pragma unroll
-            for (int i = 0; i < TM; i++) a[i] = A::fragment(stage, wm + 16 * i, half, lane);
+        for (int i = 0; i < TM; i++)
 #pragma unroll
-            for (int i = 0; i < TM; i++)
+            for (int j = 0; j < TN; j++) acc[i][j] = Element<T>::mfma(f.b[j], f.a[i], acc[i][j]);
+    }
+    // Spreads LDS reads and loads from memory between the matrix instructions of a half step.
+    template <int READS, int LOADS>
+    static __device__ __forceinline__ void interleave()
+    {
+        constexpr int kProducts = TM * TN * Element<T>::kProducts;
+        constexpr int kSlots = kProducts < 16 ? kProducts : 16;
 #pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = Element<T>::mfma(b[j], a[i], acc[i][j]);
+        for (int k = 0; k < kSlots; k++) {
+            if (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, (READS + kSlots - 1) / kSlots, 0);
+            if (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x20, (LOADS + kSlots - 1) / kSlots, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, kProducts / kSlots, 0);
         }
     }
+    static constexpr int kReads = TM * A::kReadsPerFragment + TN * B::kReadsPerFragment;
+
+    // One step: the products of the stage at `now`, whose first half is in f0 already.  LOAD: the step after the next one follows and
+    // is loaded into the same place; NEXT: another step follows, its first half is fetched into f0.
+    template <bool LOAD, bool NEXT>
+    __device__ __forceinline__ void step(A &a, B &b, Frags &f0, Frags &f1, const unsigned char *lds, uint32_t at, uint32_t now)
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(f1, lds + now, 1);
+        multiply(f0);
+        interleave<kReads, 0>();
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NEXT) {
+            // the next stage is here, and everybody is done reading this one
+            wait_loads_and_reads();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (LOAD) {
+                a.load(at + now, wave);
+                b.load(at + now + A::kBytes, wave);
+            }
+            fetch(f0, lds + (kStage - now), 0);
+        }
+        multiply(f1);
+        interleave<NEXT ? kReads : 0, LOAD ? A::kLoads + B::kLoads : 0>();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    static __device__ __forceinline__ void wait_loads_and_reads() { __builtin_amdgcn_s_waitcnt(0x0070); }
 
     // steps: of kDepth each; the last one has `last` elements of the summed axis (kRowContiguous sides).
-    __device__ __forceinline__ void run(A &a, B &b, int64_t steps, int last, unsigned char *lds)
+    // Two stages in LDS: the loads that fill one are issued half a step after its last read, a whole step before they are waited for.
+    __device__ __forceinline__ void run(A &a, B &b, int steps, int last, unsigned char *lds)
     {
         const int tid = int(threadIdx.x);
         wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -198,46 +252,58 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (steps <= 0) return;
-        if (steps == 1 && last < kDepth) {
-            a.clamp_depth(last, tid);
-            b.clamp_depth(last, tid);
-        }
-        a.load(lds, wave);
-        b.load(lds + A::kBytes, wave);
-        unsigned char *now = lds, *next = lds + kStage;
-        for (int64_t s = 0; s < steps; s++) {
-            // the stage is here, and everybody is done with the other one
-            __builtin_amdgcn_s_waitcnt(0x0f70);
-            __syncthreads();
-            if (s + 1 < steps) {
-                if (s + 2 == steps && last < kDepth) {
-                    a.clamp_depth(last, tid);
-                    b.clamp_depth(last, tid);
-                }
-                a.load(next, wave);
-                b.load(next + A::kBytes, wave);
+        const auto shorten = [&] {
+            if (last < kDepth) {
+                a.clamp_depth(last, tid);
+                b.clamp_depth(last, tid);
             }
-            multiply(now);
-            unsigned char *t = now;
-            now = next;
-            next = t;
+        };
+        const uint32_t at = lds_address(lds);
+        uint32_t now = 0;
+        if (steps == 1) shorten();
+        a.load(at, wave);
+        b.load(at + A::kBytes, wave);
+        wait_loads_and_reads();
+        __builtin_amdgcn_s_barrier();
+        if (steps > 1) {
+            if (steps == 2) shorten();
+            a.load(at + kStage, wave);
+            b.load(at + kStage + A::kBytes, wave);
         }
+        Frags f0, f1;
+        fetch(f0, lds, 0);
+        int s = 0;
+        for (; s + 3 < steps; s++) {
+            step<true, true>(a, b, f0, f1, lds, at, now);
+            now = kStage - now;
+        }
+        if (s + 2 < steps) {
+            shorten();
+            step<true, true>(a, b, f0, f1, lds, at, now);
+            now = kStage - now;
+            s++;
+        }
+        if (s + 1 < steps) {
+            step<false, true>(a, b, f0, f1, lds, at, now);
+            now = kStage - now;
+        }
+        step<false, false>(a, b, f0, f1, lds, at, now);
     }
 };
 
 // Tiles are handed out so that the blocks of one XCD (block % 8) work on neighbouring ones: within a run of tiles, bands of
 // kBand tile rows are walked column by column.
 constexpr int kXcds = 8, kBand = 4;
-__device__ __forceinline__ bool tile_of_block(int64_t block, int64_t tiles_m, int64_t tiles_n, int64_t &m, int64_t &n)
+__device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t tiles_m, uint32_t tiles_n, int &m, int &n)
 {
-    const int64_t total = tiles_m * tiles_n;
+    const uint32_t total = tiles_m * tiles_n;
     if (block >= total) return false;
-    const int64_t each = total / kXcds, more = total % kXcds, x = block % kXcds;
-    const int64_t at = x * each + (x < more ? x : more) + block / kXcds;
-    const int64_t band = at / (kBand * tiles_n), in = at % (kBand * tiles_n);
-    const int64_t high = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
-    m = band * kBand + in % high;
-    n = in / high;
+    const uint32_t each = total / kXcds, more = total % kXcds, x = block % kXcds;
+    const uint32_t at = x * each + (x < more ? x : more) + block / kXcds;
+    const uint32_t band = at / (kBand * tiles_n), in = at % (kBand * tiles_n);
+    const uint32_t high = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+    m = __builtin_amdgcn_readfirstlane(int(band * kBand + in % high));
+    n = __builtin_amdgcn_readfirstlane(int(in / high));
     return true;
 }
 
