@@ -54,7 +54,9 @@ int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad,
     if (grad) {
         at = shared;
         l.delta = take(l.rows * l.piece * size);
-        l.sums = take(l.rows * l.pitch * 4);
+        // (whole tiles of the blocks that a split sum fills, or all rows)
+        const int64_t split = int64_t(kHeadBlocks) * kHeadRows * kHeadRows, rows = l.rows * l.pitch;
+        l.sums = take((split > rows ? split : rows) * 4);
         end = at > end ? at : end;
     }
     l.bytes = end;

@@ -9,6 +9,7 @@
 namespace cgx {
 
 constexpr int kHeadRows = 256;                       // token rows and columns of a piece come in multiples of it (the largest tile)
+constexpr int kHeadBlocks = 256;                     // compute units: a sum is split into parts where its tiles are fewer
 constexpr size_t kHeadHeaderBytes = 256;
 
 inline size_t head_element(int dt) { return dt == CGX_F32 ? 4 : 2; }
@@ -29,13 +30,13 @@ struct HeadLayout {
     size_t place = 0;        // int32 [tokens]: row of a token, or -1
     size_t target = 0;       // int32 [rows]: -1 where the target is outside the vocabulary
     size_t lse = 0;          // float [rows]
-    size_t factor = 0;       // float [rows]: dloss under the scale
+    size_t factor = 0;       // float [rows]: dloss
     size_t picked = 0;       // float [rows]: the target's logit
     size_t hidden = 0;       // T [rows][pitch]
     size_t weight = 0;       // T [piece][pitch], where padded
-    size_t stats = 0;        // float2 [parts][rows]: largest logit of a part, and the sum of exp(logit - it)
+    size_t stats = 0;        // float2 [rows][parts]: largest logit of a part, and the sum of exp(logit - it)
     size_t delta = 0;        // T [rows][piece]: d of a piece
-    size_t sums = 0;         // float [rows][pitch]: dhidden while it is summed over pieces
+    size_t sums = 0;         // float [parts][rows][pitch]: dhidden while it is summed, in parts of the vocabulary if tokens are few
     size_t bytes = 0;
     int64_t columns(int64_t k) const { return k + 1 < pieces ? piece : vocab - (pieces - 1) * piece; }
 };

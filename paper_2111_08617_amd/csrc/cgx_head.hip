@@ -19,17 +19,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Header {
     int32_t count;           // tokens that count
-    float unscale;           // a power of two: what the products of d are multiplied by
+    float scale, unscale;    // powers of two: what lifted probabilities are multiplied by to give d, and the products of d
 };
-
-// 2^LIFT exp(x) of a logit's distance from the log-sum-exp or from a part's largest logit.  The binary32 calls take the library
-// function (1 ulp): their results are held to binary32 accuracy; for 16-bit types the hardware's exp2 is far below their own rounding.
-template <typename T, int LIFT = 0>
-__device__ __forceinline__ float exp_of(float x)
-{
-    if constexpr (sizeof(T) == 4) return expf(x);
-    else return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, float(LIFT)));
-}
 
 // The hardware's exp2 gives 0 below 2^-126; d of 16-bit types is formed from probabilities lifted by this much, which keeps those
 // down to 2^-150, and its scale takes the lift out again.
@@ -37,50 +28,99 @@ constexpr int kLift = 24;
 template <typename T>
 constexpr int lift_of = sizeof(T) == 2 ? kLift : 0;
 
+// exp(z - from), and 2^lift of it.  The binary32 calls take the library function (1 ulp): their results are held to binary32
+// accuracy; for 16-bit types the hardware's exp2 is far below their own rounding.
+template <typename T>
+__device__ __forceinline__ float exp_from(float z, float from)
+{
+    if constexpr (sizeof(T) == 4) return expf(z - from);
+    else return __builtin_amdgcn_exp2f((z - from) * kLog2e);
+}
+template <typename T>
+__device__ __forceinline__ float lifted(float z, float from)
+{
+    if constexpr (sizeof(T) == 4) return expf(z - from);
+    else return __builtin_amdgcn_exp2f(__builtin_fmaf(z - from, kLog2e, float(kLift)));
+}
+
 // ---------------------------------------------------------------- which tokens count
 
 // One block lists the tokens that count, in order, with their targets and factors.  A token takes part if its target is not
 // `ignore` and (gradient) its factor is not 0; the products then run over that list alone.
-// Each thread takes a run of neighbouring tokens; a prefix sum over the threads' counts gives the places.
-constexpr int kListThreads = 1024;
+// Batches of 8192 tokens: eight loads in flight per thread, a count per wave and load by vote, a prefix sum over the 128 of them.
+constexpr int kListThreads = 1024, kListWaves = kListThreads / 64, kListEach = 8;
 
 __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__restrict__ targets, const float *__restrict__ dloss,
-                                                            const float *__restrict__ lse_in, int64_t tokens, int64_t rows,
-                                                            int64_t ignore, int64_t vocab, int32_t top_bits, Header *header,
+                                                            const float *__restrict__ lse_in, int64_t tokens, int64_t ignore,
+                                                            int64_t vocab, int32_t top_bits, Header *header,
                                                             int32_t *__restrict__ index, int32_t *__restrict__ place,
                                                             int32_t *__restrict__ target, float *__restrict__ lse,
                                                             float *__restrict__ factor)
 {
-    __shared__ int32_t counts[kListThreads / 64];
-    __shared__ float tops[kListThreads / 64];
+    __shared__ int32_t before[kListEach * kListWaves + 1];
+    __shared__ float tops[kListWaves];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-    const int64_t each = (tokens + kListThreads - 1) / kListThreads, first = int64_t(tid) * each;
-    const int64_t end = first + each < tokens ? first + each : tokens;
-    int32_t mine = 0;
+    int32_t done = 0;
     float top = 0.f;
-    for (int64_t t = first; t < end; t++) {
-        const float g = dloss ? dloss[t] : 1.f;
-        if (targets[t] == ignore || g == 0.f) continue;
-        mine++;
-        top = fmaxf(top, fabsf(g));
-    }
-    int32_t before = mine;
+    for (int64_t first = 0; first < tokens; first += kListThreads * kListEach) {
+        int64_t v[kListEach];
+        float g[kListEach], l[kListEach];
+        uint64_t counts[kListEach];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int32_t other = __shfl_up(before, d, 64);
-        if (lane >= d) before += other;
-        top = fmaxf(top, __shfl_xor(top, d, 64));
+        for (int k = 0; k < kListEach; k++) {
+            const int64_t t = first + k * kListThreads + tid;
+            v[k] = t < tokens ? targets[t] : ignore;
+            g[k] = dloss && t < tokens ? dloss[t] : 1.f;
+            l[k] = dloss && t < tokens ? lse_in[t] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kListEach; k++) {
+            const bool in = v[k] != ignore && g[k] != 0.f;
+            counts[k] = __ballot(in);
+            if (in) top = fmaxf(top, fabsf(g[k]));
+            if (lane == 0) before[k * kListWaves + wave] = __popcll(counts[k]);
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const int32_t a = before[2 * lane], b = before[2 * lane + 1];
+            int32_t sum = a + b;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int32_t other = __shfl_up(sum, d, 64);
+                if (lane >= d) sum += other;
+            }
+            before[2 * lane] = sum - a - b;
+            before[2 * lane + 1] = sum - b;
+            if (lane == 63) before[kListEach * kListWaves] = sum;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kListEach; k++) {
+            const int64_t t = first + k * kListThreads + tid;
+            if (t >= tokens) continue;
+            if (!(counts[k] >> lane & 1)) {
+                place[t] = -1;
+                continue;
+            }
+            const int32_t row = done + before[k * kListWaves + wave] + __popcll(counts[k] & ((uint64_t(1) << lane) - 1));
+            const bool outside = v[k] < 0 || v[k] >= vocab;
+            index[row] = int32_t(t);
+            place[t] = row;
+            target[row] = outside ? -1 : int32_t(v[k]);
+            if (dloss) {
+                lse[row] = l[k];
+                factor[row] = outside ? __builtin_nanf("") : g[k];
+            }
+        }
+        done += before[kListEach * kListWaves];
+        __syncthreads();
     }
-    if (lane == 63) counts[wave] = before;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    int32_t count = 0;
-    before -= mine;
-    for (int w = 0; w < kListThreads / 64; w++) {
-        before += w < wave ? counts[w] : 0;
-        count += counts[w];
-        top = fmaxf(top, tops[w]);
-    }
+    if (tid != 0) return;
+    for (int w = 0; w < kListWaves; w++) top = fmaxf(top, tops[w]);
     // d is held under a power of two that moves the largest factor to [2^top_bits, 2^(top_bits + 1)): in binary16, with 14,
     // probabilities down to 1e-9 stay normal numbers and nothing overflows, whatever the loss scale
     int shift = 0;
@@ -88,25 +128,7 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
         shift = top_bits - ilogbf(top);
         shift = shift > 120 ? 120 : shift < -120 ? -120 : shift;
     }
-    const float scale = ldexpf(1.f, shift - (top_bits ? kLift : 0));
-    if (tid == 0) *header = Header{count, ldexpf(1.f, -shift)};
-    for (int64_t t = first; t < end; t++) {
-        const float g = dloss ? dloss[t] : 1.f;
-        const int64_t v = targets[t];
-        if (v == ignore || g == 0.f) {
-            place[t] = -1;
-            continue;
-        }
-        const bool outside = v < 0 || v >= vocab;
-        index[before] = int32_t(t);
-        place[t] = before;
-        target[before] = outside ? -1 : int32_t(v);
-        if (dloss) {
-            lse[before] = lse_in[t];
-            factor[before] = outside ? __builtin_nanf("") : g * scale;
-        }
-        before++;
-    }
+    *header = Header{done, ldexpf(1.f, shift - (top_bits ? kLift : 0)), ldexpf(1.f, -shift)};
 }
 
 // ---------------------------------------------------------------- rows into place
@@ -158,7 +180,7 @@ using Lds = unsigned char[K::kLds];
 // Logits of a tile, and what its rows add to their softmax: the largest logit, the sum of exp(logit - it).
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
-                                                          int64_t pitch, int64_t first, int64_t columns, int64_t rows,
+                                                          int64_t pitch, int64_t first, int64_t columns, int64_t parts,
                                                           const int32_t *__restrict__ target, float2 *__restrict__ stats,
                                                           float *__restrict__ picked)
 {
@@ -209,7 +231,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
 #pragma unroll
         for (int j = 0; j < K::TN; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) sum += exp_of<T>(tile.acc[i][j][e] - from);
+            for (int e = 0; e < 4; e++) sum += exp_from<T>(tile.acc[i][j][e], from);
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
         if (g == 0) joined[wave_n * K::BM + m] = float2{top, sum};
@@ -224,45 +246,52 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < K::WN; w++) sum += joined[w * K::BM + m].y * __builtin_amdgcn_exp2f((joined[w * K::BM + m].x - from) * kLog2e);
-        stats[((first + n0) / K::BN) * rows + m0 + m] = float2{top, sum};
+        stats[(m0 + m) * parts + (first + n0) / K::BN] = float2{top, sum};
     }
 }
 
-// Joins the parts of every token's softmax: 64 rows per block, four threads each.
-__global__ __launch_bounds__(256) void join_loss(int64_t tokens, int64_t rows, int64_t parts, const int32_t *__restrict__ place,
+// Joins the parts of every token's softmax: a wave per token.
+__global__ __launch_bounds__(256) void join_loss(int64_t tokens, int64_t parts, int64_t pitch, const int32_t *__restrict__ place,
                                                  const int32_t *__restrict__ target, const float2 *__restrict__ stats,
                                                  const float *__restrict__ picked, float *__restrict__ loss, float *__restrict__ lse)
 {
-    __shared__ float2 quarter[4][64];
-    const int at = int(threadIdx.x) & 63, q = int(threadIdx.x) >> 6;
-    const int64_t token = int64_t(blockIdx.x) * 64 + at;
-    const int32_t row = token < tokens ? place[token] : -1;
-    float top = -__builtin_inff(), sum = 0.f;
-    if (row >= 0) {
-        for (int64_t p = q; p < parts; p += 4) top = fmaxf(top, stats[p * rows + row].x);
-        const float from = top == -__builtin_inff() ? 0.f : top;
-        for (int64_t p = q; p < parts; p += 4) {
-            const float2 s = stats[p * rows + row];
-            sum += s.y * expf(s.x - from);
-        }
-    }
-    quarter[q][at] = float2{top, sum};
-    __syncthreads();
-    if (q != 0 || token >= tokens) return;
+    const int lane = int(threadIdx.x) & 63;
+    const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (token >= tokens) return;
+    const int32_t row = place[token];
     if (row < 0) {
-        loss[token] = 0.f;
-        lse[token] = 0.f;
+        if (lane == 0) loss[token] = lse[token] = 0.f;
         return;
     }
+    const float2 *s = stats + row * pitch;
+    float top = -__builtin_inff(), sum = 0.f;
+    for (int64_t first = 0; first < parts; first += 256) {
+        float2 v[4];
 #pragma unroll
-    for (int k = 1; k < 4; k++) top = fmaxf(top, quarter[k][at].x);
-    const float from = top == -__builtin_inff() ? 0.f : top;
-    sum = 0.f;
+        for (int k = 0; k < 4; k++) {
+            const int64_t p = first + 64 * k + lane;
+            v[k] = p < parts ? s[p] : float2{-__builtin_inff(), 0.f};
+        }
+        float most = top;
 #pragma unroll
-    for (int k = 0; k < 4; k++) sum += quarter[k][at].y * expf(quarter[k][at].x - from);
-    const float all = from + logf(sum);
-    lse[token] = all;
-    loss[token] = target[row] < 0 ? __builtin_nanf("") : all - picked[row];
+        for (int k = 0; k < 4; k++) most = fmaxf(most, v[k].x);
+        const float from = most == -__builtin_inff() ? 0.f : most;
+        sum *= expf(top - from);
+#pragma unroll
+        for (int k = 0; k < 4; k++) sum += v[k].y * expf(v[k].x - from);
+        top = most;
+    }
+    float all = top;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+    const float from = all == -__builtin_inff() ? 0.f : all;
+    sum *= expf(top - from);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if (lane != 0) return;
+    const float total = from + logf(sum);
+    lse[token] = total;
+    loss[token] = target[row] < 0 ? __builtin_nanf("") : total - picked[row];
 }
 
 // ---------------------------------------------------------------- gradient
@@ -279,6 +308,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
+    const float scale = header->scale;
     int tm, tn;
     if (!tile_of_block(blockIdx.x, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
@@ -289,48 +319,76 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     b.start(weight, pitch, n0, columns - n0, 0, int(threadIdx.x));
     tile.run(a, b, int(pitch / K::kDepth), K::kDepth, lds);
 
+    // Few instructions per element: this runs while the matrix cores idle.  The one element of a row that is the target's is written
+    // again afterwards, by the same lane.
     const int g = tile.lane >> 4, r = tile.lane & 15;
     const int64_t c0 = n0 + tile.wn + 4 * g;
-    const bool whole = n0 + K::BN <= columns;
+    const bool whole = m0 + K::BM <= count && n0 + K::BN <= columns;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
         const bool counts = row < count;
-        const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] : 0.f;
+        const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] * scale : 0.f;
         const int64_t hit = counts ? int64_t(target[row]) - first - c0 : -1;
+        T *const out = delta + row * piece + c0;
 #pragma unroll
         for (int j = 0; j < K::TN; j++) {
-            Four out;
+            Four v;
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float p = exp_of<T, lift_of<T>>(tile.acc[i][j][e] - base);
-                const float v = (hit == 16 * j + e ? p - float(1 << lift_of<T>) : p) * f;
-                out[e] = T(counts && (whole || c0 + 16 * j + e < columns) ? v : 0.f);
-            }
-            *reinterpret_cast<Four *>(delta + row * piece + c0 + 16 * j) = out;
+            for (int e = 0; e < 4; e++) v[e] = T(lifted<T>(tile.acc[i][j][e], base) * f);
+            if (!whole)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (!counts || c0 + 16 * j + e >= columns) v[e] = T(0.f);
+            *reinterpret_cast<Four *>(out + 16 * j) = v;
+        }
+        if (hit >= 0 && hit < 16 * K::TN && (hit & 15) < 4) {
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < K::TN; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (hit == 16 * j + e) z = tile.acc[i][j][e];
+            out[hit] = T((lifted<T>(z, base) - float(1 << lift_of<T>)) * f);
         }
     }
+}
+
+// Into how many parts the sum over a piece is split, so that the tiles of few tokens fill the chip too: as many as `blocks` allow,
+// of at least kLeastSteps steps.  Each part has sums of its own, joined by round_hidden in order.
+constexpr int kLeastSteps = 4;
+__device__ __forceinline__ uint32_t parts_of(uint32_t tiles, uint32_t steps, uint32_t blocks)
+{
+    const uint32_t most = steps / kLeastSteps, parts = tiles ? blocks / tiles : 1;
+    return parts < 1 || most < 1 ? 1 : parts < most ? parts : most;
 }
 
 // dx += d W over a piece.  accumulate: not the first piece.
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *header, const typename K::T *delta, int64_t piece,
-                                                            const typename K::T *weight, int64_t pitch, int64_t columns, int32_t accumulate,
-                                                            float *__restrict__ sums)
+                                                            const typename K::T *weight, int64_t pitch, int64_t columns, int32_t blocks,
+                                                            int32_t accumulate, float *__restrict__ sums)
 {
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
+    const uint32_t tiles_m = up(count, K::BM), tiles_n = up(pitch, K::BN), parts = parts_of(tiles_m * tiles_n, up(piece, K::kDepth), blocks);
     int tm, tn;
-    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(pitch, K::BN), tm, tn)) return;
-    const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
+    // the parts of a tile are as far apart as possible, the tiles of a part neighbours
+    if (!tile_of_block(blockIdx.x, tiles_m * parts, tiles_n, tm, tn)) return;
+    const uint32_t part = uint32_t(tm) / tiles_m;
+    const int64_t m0 = int64_t(tm - part * tiles_m) * K::BM, n0 = int64_t(tn) * K::BN;
+    const uint32_t all = up(columns, K::kDepth), each = up(all, int(parts)), from = part * each;
+    const int steps = int(from >= all ? 0 : all - from < each ? all - from : each);
     K tile;
     typename K::A a;
     typename K::B b;
-    a.start(delta, piece, m0, count - m0, 0, int(threadIdx.x));
-    b.start(weight, pitch, n0, pitch - n0, 0, int(threadIdx.x));
-    const int steps = int(up(columns, K::kDepth));
-    tile.run(a, b, steps, int(columns - int64_t(steps - 1) * K::kDepth), lds);
+    const int64_t k0 = steps ? int64_t(from) * K::kDepth : 0;
+    a.start(delta, piece, m0, count - m0, k0, int(threadIdx.x));
+    b.start(weight, pitch, n0, pitch - n0, k0, int(threadIdx.x));
+    const int64_t left = columns - k0 - int64_t(steps - 1) * K::kDepth;
+    tile.run(a, b, steps, int(left < K::kDepth ? left : K::kDepth), lds);
     const int g = tile.lane >> 4, r = tile.lane & 15;
+    float *const own = sums + int64_t(part) * count * pitch;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
@@ -339,7 +397,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
         for (int j = 0; j < K::TN; j++) {
             const int64_t column = n0 + tile.wn + 16 * j + 4 * g;
             if (column >= pitch) continue;
-            f32x4 *p = reinterpret_cast<f32x4 *>(sums + row * pitch + column);
+            f32x4 *p = reinterpret_cast<f32x4 *>(own + row * pitch + column);
             *p = accumulate ? *p + tile.acc[i][j] : tile.acc[i][j];
         }
     }
@@ -390,27 +448,33 @@ __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *hea
     }
 }
 
-// dhidden from the sums; a block per token.
+// dhidden from the sums; a block per token.  side, steps: of the kernel that left them.
 template <typename T>
 __global__ __launch_bounds__(256) void round_hidden(const Header *header, const int32_t *__restrict__ place, const float *__restrict__ sums,
-                                                    int64_t pitch, int64_t width, T *__restrict__ dhidden)
+                                                    int64_t pitch, int64_t width, int32_t side, int32_t steps, int32_t blocks,
+                                                    T *__restrict__ dhidden)
 {
     typedef T Four __attribute__((ext_vector_type(4)));
-    const int64_t token = blockIdx.x;
+    const int64_t token = blockIdx.x, count = header->count;
     const int32_t row = place[token];
     const float unscale = header->unscale;
+    const uint32_t parts = parts_of(up(count, side) * up(pitch, side), uint32_t(steps), uint32_t(blocks));
     const float *s = sums + int64_t(row < 0 ? 0 : row) * pitch;
     T *d = dhidden + token * width;
-    if (width % 4 == 0) {
-        for (int64_t k = int64_t(threadIdx.x) * 4; k < width; k += 1024) {
-            const f32x4 v = row < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4 *>(s + k);
-            Four out;
+    for (int64_t k = int64_t(threadIdx.x) * 4; k < width; k += 1024) {
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        if (row >= 0)
+            for (uint32_t p = 0; p < parts; p++) v += *reinterpret_cast<const f32x4 *>(s + int64_t(p) * count * pitch + k);
+        Four out;
 #pragma unroll
-            for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
+        for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
+        if (width % 4 == 0) {
             *reinterpret_cast<Four *>(d + k) = out;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (k + e < width) d[k + e] = out[e];
         }
-    } else {
-        for (int64_t k = int64_t(threadIdx.x); k < width; k += 256) d[k] = T(row < 0 ? 0.f : s[k] * unscale);
     }
 }
 
@@ -457,7 +521,7 @@ struct Calls {
     }
     void list(const float *dloss, const float *lse) const
     {
-        list_tokens<<<1, kListThreads, 0, stream>>>(b.targets, dloss, lse, l.tokens, l.rows, b.ignore, l.vocab,
+        list_tokens<<<1, kListThreads, 0, stream>>>(b.targets, dloss, lse, l.tokens, b.ignore, l.vocab,
                                                     l.dt == CGX_F16 ? 14 : l.dt == CGX_BF16 ? kLift : 0, header(), at<int32_t>(l.index), at<int32_t>(l.place),
                                                     at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor));
         launched();
@@ -483,7 +547,7 @@ struct Calls {
     void loss_piece(int64_t first, int64_t columns) const
     {
         loss_tiles<K><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
-            header(), hidden(), weight(first, columns), l.pitch, first, columns, l.rows, at<int32_t>(l.target), at<float2>(l.stats),
+            header(), hidden(), weight(first, columns), l.pitch, first, columns, l.parts, at<int32_t>(l.target), at<float2>(l.stats),
             at<float>(l.picked));
         launched();
     }
@@ -499,9 +563,9 @@ struct Calls {
             else loss_piece<Small<T, kSumContiguous, kSumContiguous>>(first, columns);
         }
         const int side = big ? 256 : 128;
-        join_loss<<<dim3(uint32_t((l.tokens + 63) / 64)), 256, 0, stream>>>(l.tokens, l.rows, (l.vocab + side - 1) / side,
-                                                                        at<int32_t>(l.place), at<int32_t>(l.target), at<float2>(l.stats),
-                                                                        at<float>(l.picked), loss, lse);
+        join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(l.tokens, (l.vocab + side - 1) / side, l.parts, at<int32_t>(l.place),
+                                                                      at<int32_t>(l.target), at<float2>(l.stats), at<float>(l.picked), loss,
+                                                                      lse);
         launched();
         return error;
     }
@@ -514,11 +578,23 @@ struct Calls {
             l.piece);
         launched();
     }
+    // (one block of the large tile fits a compute unit, two of the small one)
+    template <typename K>
+    static constexpr int blocks = K::BM == 256 ? kHeadBlocks : 2 * kHeadBlocks;
     template <typename K>
     void hidden_sums(const T *w, int64_t first, int64_t columns) const
     {
-        hidden_tiles<K><<<dim3(uint32_t(tiles(l.tokens, l.pitch, K::BM))), K::kThreads, 0, stream>>>(
-            header(), at<T>(l.delta), l.piece, w, l.pitch, columns, first > 0, at<float>(l.sums));
+        const int64_t n = tiles(l.tokens, l.pitch, K::BM);
+        hidden_tiles<K><<<dim3(uint32_t(n > blocks<K> ? n : blocks<K>)), K::kThreads, 0, stream>>>(
+            header(), at<T>(l.delta), l.piece, w, l.pitch, columns, blocks<K>, first > 0, at<float>(l.sums));
+        launched();
+    }
+    template <typename K>
+    void rounded(T *dhidden) const
+    {
+        round_hidden<T><<<dim3(uint32_t(l.tokens)), 256, 0, stream>>>(header(), at<int32_t>(l.place), at<float>(l.sums), l.pitch, l.width,
+                                                                   K::BM, int32_t((l.piece + K::kDepth - 1) / K::kDepth), blocks<K>,
+                                                                   dhidden);
         launched();
     }
     template <typename K>
@@ -537,17 +613,12 @@ struct Calls {
             if (l.tokens) {
                 if (large<T>(l.tokens, columns)) delta<Large<T, kSumContiguous, kSumContiguous>>(w, first, columns);
                 else delta<Small<T, kSumContiguous, kSumContiguous>>(w, first, columns);
-                if (large<T>(l.tokens, l.pitch)) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
-                else hidden_sums<Small<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
             }
             if (large<T>(columns, l.width)) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
             else weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
         }
-        if (l.tokens) {
-            round_hidden<T><<<dim3(uint32_t(l.tokens)), 256, 0, stream>>>(header(), at<int32_t>(l.place), at<float>(l.sums), l.pitch, l.width,
-                                                                       dhidden);
-            launched();
-        }
+        if (l.tokens) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
         return error;
     }
 };
