@@ -57,6 +57,7 @@ int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad,
         // (whole tiles of the blocks that a split sum fills, or all rows)
         const int64_t split = int64_t(kHeadBlocks) * kHeadRows * kHeadRows, rows = l.rows * l.pitch;
         l.sums = take((split > rows ? split : rows) * 4);
+        l.spare = take(split * 4);
         end = at > end ? at : end;
     }
     l.bytes = end;

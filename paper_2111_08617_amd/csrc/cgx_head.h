@@ -37,6 +37,7 @@ struct HeadLayout {
     size_t stats = 0;        // float2 [rows][parts]: largest logit of a part, and the sum of exp(logit - it)
     size_t delta = 0;        // T [rows][piece]: d of a piece
     size_t sums = 0;         // float [parts][rows][pitch]: dhidden while it is summed, in parts of the vocabulary if tokens are few
+    size_t spare = 0;        // float [blocks][tile]: parts of tiles of the weight's gradient
     size_t bytes = 0;
     int64_t columns(int64_t k) const { return k + 1 < pieces ? piece : vocab - (pieces - 1) * piece; }
 };

@@ -30,17 +30,18 @@ constexpr int lift_of = sizeof(T) == 2 ? kLift : 0;
 
 // exp(z - from), and 2^lift of it.  The binary32 calls take the library function (1 ulp): their results are held to binary32
 // accuracy; for 16-bit types the hardware's exp2 is far below their own rounding.
+// (`from` comes multiplied by log2 e: its rounding moves all terms of a row alike, by less than the rounding of the row's lse.)
 template <typename T>
 __device__ __forceinline__ float exp_from(float z, float from)
 {
     if constexpr (sizeof(T) == 4) return expf(z - from);
-    else return __builtin_amdgcn_exp2f((z - from) * kLog2e);
+    else return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -(from * kLog2e)));
 }
 template <typename T>
 __device__ __forceinline__ float lifted(float z, float from)
 {
     if constexpr (sizeof(T) == 4) return expf(z - from);
-    else return __builtin_amdgcn_exp2f(__builtin_fmaf(z - from, kLog2e, float(kLift)));
+    else return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, __builtin_fmaf(-from, kLog2e, float(kLift))));
 }
 
 // ---------------------------------------------------------------- which tokens count
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
     int tm, tn;
-    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
+    if (!tile_of_block(blockIdx.x, ~0u, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     K tile;
     typename K::A a;
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
     __syncthreads();
     float2 *joined = reinterpret_cast<float2 *>(lds);        // [WN][BM]
     const int g = tile.lane >> 4, r = tile.lane & 15, wave_n = tile.wave % K::WN;
-    const int64_t c0 = n0 + tile.wn + 4 * g;
+    const int64_t c0 = n0 + tile.wn + 16 * g;
     const bool whole = n0 + K::BN <= columns;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
@@ -208,12 +209,12 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
         const int64_t row = m0 + m;
         if (row < count) {
             const int64_t d = int64_t(target[row]) - first - c0;
-            if (d >= 0 && d < 16 * K::TN && (d & 15) < 4) {
+            if (d >= 0 && d < 16) {
 #pragma unroll
                 for (int j = 0; j < K::TN; j++)
 #pragma unroll
                     for (int e = 0; e < 4; e++)
-                        if (d == 16 * j + e) picked[row] = tile.acc[i][j][e];
+                        if (d == 4 * j + e) picked[row] = tile.acc[i][j][e];
             }
         }
         float top = -__builtin_inff();
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
         for (int j = 0; j < K::TN; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                if (!whole && c0 + 16 * j + e >= columns) tile.acc[i][j][e] = -__builtin_inff();
+                if (!whole && c0 + 4 * j + e >= columns) tile.acc[i][j][e] = -__builtin_inff();
                 top = fmaxf(top, tile.acc[i][j][e]);
             }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -305,12 +306,11 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
                                                            const float *__restrict__ factor, typename K::T *__restrict__ delta, int64_t piece)
 {
     using T = typename K::T;
-    typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
     const float scale = header->scale;
     int tm, tn;
-    if (!tile_of_block(blockIdx.x, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
+    if (!tile_of_block(blockIdx.x, ~0u, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
     K tile;
     typename K::A a;
@@ -322,8 +322,10 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     // Few instructions per element: this runs while the matrix cores idle.  The one element of a row that is the target's is written
     // again afterwards, by the same lane.
     const int g = tile.lane >> 4, r = tile.lane & 15;
-    const int64_t c0 = n0 + tile.wn + 4 * g;
+    const int64_t c0 = n0 + tile.wn + 16 * g;
     const bool whole = m0 + K::BM <= count && n0 + K::BN <= columns;
+    constexpr int kPer = 16 / int(sizeof(T));
+    typedef T Vec __attribute__((ext_vector_type(kPer)));
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
@@ -332,23 +334,21 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
         const int64_t hit = counts ? int64_t(target[row]) - first - c0 : -1;
         T *const out = delta + row * piece + c0;
 #pragma unroll
-        for (int j = 0; j < K::TN; j++) {
-            Four v;
+        for (int k = 0; k < 16; k += kPer) {
+            Vec v;
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = T(lifted<T>(tile.acc[i][j][e], base) * f);
+            for (int e = 0; e < kPer; e++) v[e] = T(lifted<T>(tile.acc[i][(k + e) / 4][(k + e) % 4], base) * f);
             if (!whole)
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (!counts || c0 + 16 * j + e >= columns) v[e] = T(0.f);
-            *reinterpret_cast<Four *>(out + 16 * j) = v;
+                for (int e = 0; e < kPer; e++)
+                    if (!counts || c0 + k + e >= columns) v[e] = T(0.f);
+            *reinterpret_cast<Vec *>(out + k) = v;
         }
-        if (hit >= 0 && hit < 16 * K::TN && (hit & 15) < 4) {
+        if (hit >= 0 && hit < 16) {
             float z = 0.f;
 #pragma unroll
-            for (int j = 0; j < K::TN; j++)
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (hit == 16 * j + e) z = tile.acc[i][j][e];
+            for (int k = 0; k < 16; k++)
+                if (hit == k) z = tile.acc[i][k / 4][k % 4];
             out[hit] = T((lifted<T>(z, base) - float(1 << lift_of<T>)) * f);
         }
     }
@@ -374,7 +374,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
     const uint32_t tiles_m = up(count, K::BM), tiles_n = up(pitch, K::BN), parts = parts_of(tiles_m * tiles_n, up(piece, K::kDepth), blocks);
     int tm, tn;
     // the parts of a tile are as far apart as possible, the tiles of a part neighbours
-    if (!tile_of_block(blockIdx.x, tiles_m * parts, tiles_n, tm, tn)) return;
+    if (!tile_of_block(blockIdx.x, ~0u, tiles_m * parts, tiles_n, tm, tn)) return;
     const uint32_t part = uint32_t(tm) / tiles_m;
     const int64_t m0 = int64_t(tm - part * tiles_m) * K::BM, n0 = int64_t(tn) * K::BN;
     const uint32_t all = up(columns, K::kDepth), each = up(all, int(parts)), from = part * each;
@@ -403,48 +403,112 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
     }
 }
 
-// dW = d^T x for the rows of a piece.
+// dW = d^T x for the rows of a piece.  The tiles fill the chip's compute units some number of times; those of the last, partial round are
+// split over the tokens into as many parts as fill it, each part with sums of its own (`spare`, by part and tile), which weight_rest
+// joins.  (Without that, 50257 x 2048 weights in two pieces took 4 rounds each for 3.06 rounds' work.)
+struct Rounds {
+    uint32_t whole;          // tiles that a block computes alone
+    uint32_t rest;           // tiles of the last round
+    uint32_t parts;          // of each of these
+};
+__device__ __forceinline__ Rounds rounds_of(uint32_t tiles, uint32_t steps, uint32_t blocks)
+{
+    const uint32_t whole = tiles / blocks * blocks, rest = tiles - whole, most = steps / kLeastSteps;
+    uint32_t parts = rest ? blocks / rest : 1;
+    parts = parts < most ? parts : most;
+    return parts < 2 ? Rounds{tiles, 0, 1} : Rounds{whole, rest, parts};
+}
+
+template <typename T>
+__device__ __forceinline__ void store_weights(T *dweight, int64_t row, int64_t column, int64_t width, f32x4 v, float unscale)
+{
+    typedef T Four __attribute__((ext_vector_type(4)));
+    Four out;
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
+    T *p = dweight + row * width + column;
+    if (width % 4 == 0) {
+        *reinterpret_cast<Four *>(p) = out;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (column + e < width) p[e] = out[e];
+    }
+}
+
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *header, const typename K::T *delta, int64_t piece,
                                                             Hidden<typename K::T> hidden, int64_t pitch, int64_t columns, int64_t width,
-                                                            typename K::T *__restrict__ dweight)
+                                                            int32_t blocks, typename K::T *__restrict__ dweight, float *__restrict__ spare)
 {
-    using T = typename K::T;
-    typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
+    const uint32_t tiles_m = up(columns, K::BM), tiles_n = up(width, K::BN), all = up(count, K::kDepth);
+    const Rounds r = rounds_of(tiles_m * tiles_n, all, uint32_t(blocks));
+    uint32_t from = 0, steps = all, part = 0, tile_at = blockIdx.x;
+    const bool shared = blockIdx.x >= r.whole;
+    if (shared) {
+        const uint32_t at = blockIdx.x - r.whole;
+        if (at >= r.rest * r.parts) return;
+        part = at / r.rest;
+        tile_at = r.whole + at % r.rest;
+        const uint32_t each = up(all, int(r.parts));
+        from = part * each;
+        steps = from >= all ? 0 : all - from < each ? all - from : each;
+        if (!steps) from = 0;
+    }
     int tm, tn;
-    if (!tile_of_block(blockIdx.x, up(columns, K::BM), up(width, K::BN), tm, tn)) return;
+    if (!tile_of_block(tile_at, r.whole, tiles_m, tiles_n, tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
-    const float unscale = header->unscale;
     K tile;
     typename K::A a;
     typename K::B b;
-    a.start(delta, piece, m0, piece - m0, 0, int(threadIdx.x));
-    b.start(hidden.of(count), pitch, n0, pitch - n0, 0, int(threadIdx.x));
-    tile.run(a, b, int(up(count, K::kDepth)), K::kDepth, lds);
-    const int g = tile.lane >> 4, r = tile.lane & 15;
-    const bool fours = width % 4 == 0;
+    a.start(delta, piece, m0, piece - m0, int64_t(from) * K::kDepth, int(threadIdx.x));
+    b.start(hidden.of(count), pitch, n0, pitch - n0, int64_t(from) * K::kDepth, int(threadIdx.x));
+    tile.run(a, b, int(steps), K::kDepth, lds);
+    const int g = tile.lane >> 4, l = tile.lane & 15;
+    if (shared) {
+        float *own = spare + int64_t(blockIdx.x - r.whole) * (K::BM * K::BN);
+#pragma unroll
+        for (int i = 0; i < K::TM; i++)
+#pragma unroll
+            for (int j = 0; j < K::TN; j++)
+                *reinterpret_cast<f32x4 *>(own + (tile.wm + 16 * i + l) * K::BN + tile.wn + 16 * j + 4 * g) = tile.acc[i][j];
+        return;
+    }
+    const float unscale = header->unscale;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
-        const int64_t row = m0 + tile.wm + 16 * i + r;
+        const int64_t row = m0 + tile.wm + 16 * i + l;
         if (row >= columns) continue;
 #pragma unroll
         for (int j = 0; j < K::TN; j++) {
             const int64_t column = n0 + tile.wn + 16 * j + 4 * g;
-            if (column >= width) continue;
-            T *p = dweight + row * width + column;
-            Four out;
-#pragma unroll
-            for (int e = 0; e < 4; e++) out[e] = T(tile.acc[i][j][e] * unscale);
-            if (fours) {
-                *reinterpret_cast<Four *>(p) = out;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (column + e < width) p[e] = out[e];
-            }
+            if (column < width) store_weights(dweight, row, column, width, tile.acc[i][j], unscale);
         }
+    }
+}
+
+// The tiles of weight_tiles' last round from their parts: a block per 16 rows of a tile.
+template <typename K>
+__global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t columns, int64_t width, int32_t blocks,
+                                                   typename K::T *__restrict__ dweight, const float *__restrict__ spare)
+{
+    constexpr int kStrip = 16;
+    const uint32_t tiles_m = up(columns, K::BM), tiles_n = up(width, K::BN);
+    const Rounds r = rounds_of(tiles_m * tiles_n, up(header->count, K::kDepth), uint32_t(blocks));
+    const uint32_t at = blockIdx.x / (K::BM / kStrip), strip = blockIdx.x % (K::BM / kStrip);
+    int tm, tn;
+    if (at >= r.rest || !tile_of_block(r.whole + at, r.whole, tiles_m, tiles_n, tm, tn)) return;
+    const float unscale = header->unscale;
+    for (int k = int(threadIdx.x) * 4; k < kStrip * K::BN; k += 1024) {
+        const int m = int(strip) * kStrip + k / K::BN, n = k % K::BN;
+        const int64_t row = int64_t(tm) * K::BM + m, column = int64_t(tn) * K::BN + n;
+        if (row >= columns || column >= width) continue;
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        for (uint32_t p = 0; p < r.parts; p++)
+            v += *reinterpret_cast<const f32x4 *>(spare + (int64_t(p) * r.rest + at) * (K::BM * K::BN) + m * K::BN + n);
+        store_weights(dweight, row, column, width, v, unscale);
     }
 }
 
@@ -507,6 +571,9 @@ struct Calls {
         if (error == hipSuccess) error = e;
     }
 
+    // Blocks that the chip holds at a time: one of the large tile per compute unit, two of the small one.
+    template <typename K>
+    static constexpr int blocks = K::BM == 256 ? kHeadBlocks : 2 * kHeadBlocks;
     template <typename U>
     U *at(size_t offset) const
     {
@@ -559,8 +626,8 @@ struct Calls {
         const bool big = large<T>(l.tokens, piece);
         for (int64_t first = 0; first < l.vocab; first += piece) {
             const int64_t columns = l.vocab - first < piece ? l.vocab - first : piece;
-            if (big) loss_piece<Large<T, kSumContiguous, kSumContiguous>>(first, columns);
-            else loss_piece<Small<T, kSumContiguous, kSumContiguous>>(first, columns);
+            if (big) loss_piece<Large<T, kSumContiguous, kSumStrips>>(first, columns);
+            else loss_piece<Small<T, kSumContiguous, kSumStrips>>(first, columns);
         }
         const int side = big ? 256 : 128;
         join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(l.tokens, (l.vocab + side - 1) / side, l.parts, at<int32_t>(l.place),
@@ -578,9 +645,6 @@ struct Calls {
             l.piece);
         launched();
     }
-    // (one block of the large tile fits a compute unit, two of the small one)
-    template <typename K>
-    static constexpr int blocks = K::BM == 256 ? kHeadBlocks : 2 * kHeadBlocks;
     template <typename K>
     void hidden_sums(const T *w, int64_t first, int64_t columns) const
     {
@@ -600,8 +664,14 @@ struct Calls {
     template <typename K>
     void weight_rows(int64_t first, int64_t columns, T *dweight) const
     {
-        weight_tiles<K><<<dim3(uint32_t(tiles(columns, l.width, K::BM))), K::kThreads, 0, stream>>>(
-            header(), at<T>(l.delta), l.piece, hidden(), l.pitch, columns, l.width, dweight + first * l.width);
+        const int64_t n = tiles(columns, l.width, K::BM), rest = n % blocks<K>;
+        // (whether the rest is split depends on how many tokens count, too)
+        weight_tiles<K><<<dim3(uint32_t(n - rest + (rest ? blocks<K> : 0))), K::kThreads, 0, stream>>>(
+            header(), at<T>(l.delta), l.piece, hidden(), l.pitch, columns, l.width, blocks<K>, dweight + first * l.width, at<float>(l.spare));
+        launched();
+        if (!rest || 2 * rest > blocks<K> || (l.tokens + K::kDepth - 1) / K::kDepth < 2 * kLeastSteps) return;
+        weight_rest<K><<<dim3(uint32_t(rest * (K::BM / 16))), 256, 0, stream>>>(header(), columns, l.width, blocks<K>,
+                                                                             dweight + first * l.width, at<float>(l.spare));
         launched();
     }
     hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight) const
@@ -611,8 +681,8 @@ struct Calls {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
             if (l.tokens) {
-                if (large<T>(l.tokens, columns)) delta<Large<T, kSumContiguous, kSumContiguous>>(w, first, columns);
-                else delta<Small<T, kSumContiguous, kSumContiguous>>(w, first, columns);
+                if (large<T>(l.tokens, columns)) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                else delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
             }
             if (large<T>(columns, l.width)) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);

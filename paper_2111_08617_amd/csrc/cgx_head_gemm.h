@@ -50,6 +50,7 @@ struct Element<float> {
 // An operand of the product C[m][n] = sum_k A(m, k) B(n, k).
 enum Layout {
     kSumContiguous,      // element (row, k) at row * pitch + k
+    kSumStrips,          // the same, read in strips of 64 rows: fragment j holds rows 4 j .. 4 j + 3 of each 16 of the strip
     kRowContiguous       // element (row, k) at k * pitch + row
 };
 
@@ -76,8 +77,8 @@ struct Side {
     static constexpr int kLoads = kPieces / THREADS;
     static constexpr int kBytes = ROWS * kStepBytes;
     static_assert(kPieces % THREADS == 0 && ROWS % kMnUnit == 0, "a tile side is filled by whole instructions");
-    static constexpr int kReadsPerFragment = LAYOUT == kSumContiguous ? 1 : sizeof(T) == 2 ? 2 : 4;
-    static constexpr int kPiecesPerRow = LAYOUT == kSumContiguous ? kStepBytes / 16 : ROWS / kPer;
+    static constexpr int kReadsPerFragment = LAYOUT != kRowContiguous ? 1 : sizeof(T) == 2 ? 2 : 4;
+    static constexpr int kPiecesPerRow = LAYOUT != kRowContiguous ? kStepBytes / 16 : ROWS / kPer;
 
     const T *base;            // of the current step, uniform
     int64_t pitch;
@@ -90,17 +91,18 @@ struct Side {
     {
         const int row = stored_row(q), piece = q % kPiecesPerRow;
         if constexpr (LAYOUT == kSumContiguous) return piece ^ ((row >> 1) & 7);
+        else if constexpr (LAYOUT == kSumStrips) return piece ^ (((row >> 1) & 1) | ((row >> 3) & 6));
         else if constexpr (sizeof(T) == 2) return piece ^ (((row & 3) | ((row >> 1) & 4)) << 1);
         else return piece ^ (((row >> 2) & 3) << 2);
     }
 
     // rows: how many rows exist from row0 on; those past the end are read from the last ones, and their results are not used.
     // depth: how much of the summed axis exists; a kRowContiguous side re-reads its last row past it (the other side holds
-    // zeros there), a kSumContiguous one has to be readable up to a whole step.
+    // zeros there), the others have to be readable up to a whole step.
     __device__ __forceinline__ void start(const T *all, int64_t pitch_, int64_t row0, int64_t rows, int64_t k0, int tid)
     {
         pitch = pitch_;
-        if constexpr (LAYOUT == kSumContiguous) {
+        if constexpr (LAYOUT != kRowContiguous) {
             base = all + row0 * pitch + k0;
             step = kDepth;
         } else {
@@ -111,7 +113,7 @@ struct Side {
         for (int i = 0; i < kLoads; i++) {
             const int q = i * THREADS + tid;
             int row = stored_row(q), piece = source_piece(q);
-            if constexpr (LAYOUT == kSumContiguous) row = row < rows ? row : int(rows) - 1;
+            if constexpr (LAYOUT != kRowContiguous) row = row < rows ? row : int(rows) - 1;
             else piece = (piece + 1) * kPer <= rows ? piece : int(rows) / kPer - 1;
             offset[i] = uint32_t((uint32_t(row) * uint32_t(pitch) + uint32_t(piece) * kPer) * sizeof(T));
         }
@@ -133,12 +135,15 @@ struct Side {
         for (int i = 0; i < kLoads; i++) to_lds(b, offset[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
         base += step;
     }
-    // The fragment of rows row0 .. row0 + 15 (row0 a multiple of 16) and the half-th 64 bytes of the step.
-    static __device__ __forceinline__ typename Element<T>::Frag fragment(const unsigned char *lds, int row0, int half, int lane)
+    // Fragment j of the rows from `first` on (a multiple of 64 for strips, of 16 otherwise): 16 rows, the half-th 64 bytes of the step.
+    static __device__ __forceinline__ typename Element<T>::Frag fragment(const unsigned char *lds, int first, int j, int half, int lane)
     {
         using Frag = typename Element<T>::Frag;
-        const int g = lane >> 4, r = lane & 15;
-        if constexpr (LAYOUT == kSumContiguous) {
+        const int g = lane >> 4, r = lane & 15, row0 = first + 16 * j;
+        if constexpr (LAYOUT == kSumStrips) {
+            const int row = first + 16 * (r >> 2) + 4 * j + (r & 3);
+            return *reinterpret_cast<const Frag *>(lds + row * kStepBytes + (((half * 4 + g) ^ (((r >> 1) & 1) | ((r >> 1) & 6))) << 4));
+        } else if constexpr (LAYOUT == kSumContiguous) {
             return *reinterpret_cast<const Frag *>(lds + (row0 + r) * kStepBytes + (((half * 4 + g) ^ (r >> 1)) << 4));
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes read a 4 x 16 block of 16-bit elements and get it transposed: four elements of the summed axis each
@@ -162,7 +167,8 @@ struct Side {
 
 // A tile of C of BM x BN elements by WM x WN waves.  A lane ends with acc[i][j][e] = C[m][n] for
 //   m = 16 i + lane % 16 (+ the wave's first row), n = 16 j + 4 (lane / 16) + e (+ the wave's first column):
-// four neighbouring columns of a row (the side of the columns is the instruction's first operand).
+// four neighbouring columns of a row (the side of the columns is the instruction's first operand).  With kSumStrips columns
+// n = 16 (lane / 16) + 4 j + e: sixteen neighbouring ones, which an epilogue of 16-bit elements stores 16 bytes at a time.
 template <typename T_, int BM_, int BN_, int WM_, int WN_, Layout LA, Layout LB>
 struct Tile {
     using T = T_;
@@ -172,6 +178,7 @@ struct Tile {
     using B = Side<T, LB, BN, kThreads>;
     static constexpr int kDepth = A::kDepth;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    static_assert(LB != kSumStrips || TN == 4, "strips are as wide as a wave's columns");
     static constexpr int kStage = A::kBytes + B::kBytes;
     static constexpr int kLds = 2 * kStage;
 
@@ -185,9 +192,9 @@ struct Tile {
     __device__ __forceinline__ void fetch(Frags &f, const unsigned char *stage, int half) const
     {
 #pragma unroll
-        for (int j = 0; j < TN; j++) f.b[j] = B::fragment(stage + A::kBytes, wn + 16 * j, half, lane);
+        for (int j = 0; j < TN; j++) f.b[j] = B::fragment(stage + A::kBytes, wn, j, half, lane);
 #pragma unroll
-        for (int i = 0; i < TM; i++) f.a[i] = A::fragment(stage, wm + 16 * i, half, lane);
+        for (int i = 0; i < TM; i++) f.a[i] = A::fragment(stage, wm, i, half, lane);
     }
     __device__ __forceinline__ void multiply(const Frags &f)
     {
@@ -292,14 +299,18 @@ struct Tile {
 };
 
 // Tiles are handed out so that the blocks of one XCD (block % 8) work on neighbouring ones: within a run of tiles, bands of
-// kBand tile rows are walked column by column.
+// kBand tile rows are walked column by column.  Of the first `whole` blocks, that is (all of them, if there are more); any others
+// take the tiles that follow, in order.
 constexpr int kXcds = 8, kBand = 4;
-__device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t tiles_m, uint32_t tiles_n, int &m, int &n)
+__device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t whole, uint32_t tiles_m, uint32_t tiles_n, int &m, int &n)
 {
-    const uint32_t total = tiles_m * tiles_n;
-    if (block >= total) return false;
-    const uint32_t each = total / kXcds, more = total % kXcds, x = block % kXcds;
-    const uint32_t at = x * each + (x < more ? x : more) + block / kXcds;
+    const uint32_t all = tiles_m * tiles_n, total = whole < all ? whole : all;
+    if (block >= all) return false;
+    uint32_t at = block;
+    if (block < total) {
+        const uint32_t each = total / kXcds, more = total % kXcds, x = block % kXcds;
+        at = x * each + (x < more ? x : more) + block / kXcds;
+    }
     const uint32_t band = at / (kBand * tiles_n), in = at % (kBand * tiles_n);
     const uint32_t high = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
     m = __builtin_amdgcn_readfirstlane(int(band * kBand + in % high));

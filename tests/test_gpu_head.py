@@ -266,3 +266,12 @@ def test_captured_into_a_graph(torch):
         torch.cuda.synchronize()
         assert torch.equal(loss, want["loss"]) and torch.equal(lse, want["lse"])
         assert torch.equal(dh, want["dhidden"]) and torch.equal(dw, want["dweight"])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens", [447, 448, 449, 480, 512, 513, 1100])
+def test_the_last_round_of_the_weights_tiles(torch, tokens, dtype):
+    """260 tiles of the weight's gradient: four more than the chip takes at once, split over the tokens where these are enough."""
+    hidden, weight, targets = inputs(torch, tokens, 1024, 16640 - 3, dtype, seed=tokens)
+    targets[5::9] = -100
+    check(torch, hidden, weight, targets, torch.full((tokens,), 1.0 / tokens, device="cuda"))
