@@ -544,18 +544,24 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
 
 // ---------------------------------------------------------------- launches
 
+// Three tiles.  The large one reads each operand least often; the smaller ones fill the chip's 256 compute units (one, two and four blocks
+// each) where there are few of it, or where the tokens do not fill its rows.
+template <typename T, Layout LA, Layout LB>
+using Tiny = Tile<T, 64, 64, 4, 1, LA, LB>;
 template <typename T, Layout LA, Layout LB>
 using Small = Tile<T, 128, 128, 2, 2, LA, LB>;
+// (binary32 products are bound by the matrix cores, which the small tile keeps as busy)
 template <typename T, Layout LA, Layout LB>
 using Large = std::conditional_t<sizeof(T) == 2, Tile<T, 256, 256, 2, 4, LA, LB>, Small<T, LA, LB>>;
 
 int64_t tiles(int64_t rows, int64_t columns, int side) { return ((rows + side - 1) / side) * ((columns + side - 1) / side); }
 
-// The large tile reads each operand half as often, the small one fills the chip's 256 compute units from a quarter of the size.
+enum Size { kTiny, kSmall, kLarge };
 template <typename T>
-bool large(int64_t rows, int64_t columns)
+Size size_of(int64_t rows, int64_t columns)
 {
-    return sizeof(T) == 2 && tiles(rows, columns, 256) >= 192;
+    if (sizeof(T) == 2 && rows > 128 && tiles(rows, columns, 256) >= 192) return kLarge;
+    return rows > 64 && tiles(rows, columns, 128) >= 192 ? kSmall : kTiny;
 }
 
 template <typename T>
@@ -571,9 +577,9 @@ struct Calls {
         if (error == hipSuccess) error = e;
     }
 
-    // Blocks that the chip holds at a time: one of the large tile per compute unit, two of the small one.
+    // Blocks that the chip holds at a time: one of the large tile per compute unit, two of the small one, four of the tiny one.
     template <typename K>
-    static constexpr int blocks = K::BM == 256 ? kHeadBlocks : 2 * kHeadBlocks;
+    static constexpr int blocks = K::BM == 256 ? kHeadBlocks : K::BM == 128 ? 2 * kHeadBlocks : 4 * kHeadBlocks;
     template <typename U>
     U *at(size_t offset) const
     {
@@ -623,13 +629,14 @@ struct Calls {
         list(nullptr, nullptr);
         // (a weight that needs no padding is walked in one launch)
         const int64_t piece = l.padded ? l.piece : l.vocab;
-        const bool big = large<T>(l.tokens, piece);
+        const Size size = size_of<T>(l.tokens, piece);
         for (int64_t first = 0; first < l.vocab; first += piece) {
             const int64_t columns = l.vocab - first < piece ? l.vocab - first : piece;
-            if (big) loss_piece<Large<T, kSumContiguous, kSumStrips>>(first, columns);
-            else loss_piece<Small<T, kSumContiguous, kSumStrips>>(first, columns);
+            if (size == kLarge) loss_piece<Large<T, kSumContiguous, kSumStrips>>(first, columns);
+            else if (size == kSmall) loss_piece<Small<T, kSumContiguous, kSumStrips>>(first, columns);
+            else loss_piece<Tiny<T, kSumContiguous, kSumStrips>>(first, columns);
         }
-        const int side = big ? 256 : 128;
+        const int side = size == kLarge ? 256 : size == kSmall ? 128 : 64;
         join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(l.tokens, (l.vocab + side - 1) / side, l.parts, at<int32_t>(l.place),
                                                                       at<int32_t>(l.target), at<float2>(l.stats), at<float>(l.picked), loss,
                                                                       lse);
@@ -677,18 +684,26 @@ struct Calls {
     hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight) const
     {
         list(dloss, lse);
+        // (sums over the vocabulary are split where they have few tiles: tiles of few tokens' rows need only be no larger than these)
+        const bool wide = l.tokens > 64;
         for (int64_t k = 0; k < l.pieces; k++) {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
             if (l.tokens) {
-                if (large<T>(l.tokens, columns)) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                else delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                const Size size = size_of<T>(l.tokens, columns);
+                if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                if (wide) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                else hidden_sums<Tiny<T, kSumContiguous, kRowContiguous>>(w, first, columns);
             }
-            if (large<T>(columns, l.width)) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
-            else weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            const Size size = size_of<T>(columns, l.width);
+            if (size == kLarge) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            else if (size == kSmall) weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            else weight_rows<Tiny<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
         }
-        if (l.tokens) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
+        if (l.tokens && wide) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
+        else if (l.tokens) rounded<Tiny<T, kSumContiguous, kRowContiguous>>(dhidden);
         return error;
     }
 };

@@ -17,7 +17,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStepBytes = 128;      // bytes of the summed axis that one step of the main loop takes per row
-constexpr int kMnUnit = 128;         // elements that a tile side must be a multiple of
+constexpr int kMnUnit = 64;          // elements that a tile side must be a multiple of
 
 // What a lane feeds the matrix cores at once: 16 bytes of consecutive elements of the summed axis.  Four groups of 16 lanes
 // make 64 bytes of it; one or (binary32) four instructions consume them.
@@ -77,6 +77,7 @@ struct Side {
     static constexpr int kLoads = kPieces / THREADS;
     static constexpr int kBytes = ROWS * kStepBytes;
     static_assert(kPieces % THREADS == 0 && ROWS % kMnUnit == 0, "a tile side is filled by whole instructions");
+    static constexpr int kUnits = ROWS / 16 - 1 < 7 ? ROWS / 16 - 1 : 7;   // of 32 bytes, that the rows of 16-bit elements are permuted among
     static constexpr int kReadsPerFragment = LAYOUT != kRowContiguous ? 1 : sizeof(T) == 2 ? 2 : 4;
     static constexpr int kPiecesPerRow = LAYOUT != kRowContiguous ? kStepBytes / 16 : ROWS / kPer;
 
@@ -92,7 +93,7 @@ struct Side {
         const int row = stored_row(q), piece = q % kPiecesPerRow;
         if constexpr (LAYOUT == kSumContiguous) return piece ^ ((row >> 1) & 7);
         else if constexpr (LAYOUT == kSumStrips) return piece ^ (((row >> 1) & 1) | ((row >> 3) & 6));
-        else if constexpr (sizeof(T) == 2) return piece ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+        else if constexpr (sizeof(T) == 2) return piece ^ ((((row & 3) | ((row >> 1) & 4)) & kUnits) << 1);
         else return piece ^ (((row >> 2) & 3) << 2);
     }
 
@@ -147,7 +148,7 @@ struct Side {
             return *reinterpret_cast<const Frag *>(lds + (row0 + r) * kStepBytes + (((half * 4 + g) ^ (r >> 1)) << 4));
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes read a 4 x 16 block of 16-bit elements and get it transposed: four elements of the summed axis each
-            const int unit = (row0 >> 4) ^ ((r >> 2) | ((g & 1) << 2));
+            const int unit = (row0 >> 4) ^ (((r >> 2) | ((g & 1) << 2)) & kUnits);
             const unsigned char *p = lds + (half * 32 + g * 8 + (r >> 2)) * (ROWS * 2) + unit * 32 + (r & 3) * 8;
             using Lds4 = __attribute__((address_space(3))) s16x4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4 *)p);
@@ -208,7 +209,7 @@ struct Tile {
     static __device__ __forceinline__ void interleave()
     {
         constexpr int kProducts = TM * TN * Element<T>::kProducts;
-        constexpr int kSlots = kProducts < 16 ? kProducts : 16;
+        constexpr int kSlots = kProducts < 16 ? kProducts : 16;      // (every one has a product)
 #pragma unroll
         for (int k = 0; k < kSlots; k++) {
             if (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, (READS + kSlots - 1) / kSlots, 0);
