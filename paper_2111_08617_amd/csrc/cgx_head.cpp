@@ -39,7 +39,6 @@ int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad,
         at += size_t(up(bytes, 256));
         return here;
     };
-    l.index = take(l.rows * 4);
     l.place = take(tokens * 4);
     l.target = take(l.rows * 4);
     l.lse = take(l.rows * 4);

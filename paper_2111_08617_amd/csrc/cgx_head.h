@@ -26,8 +26,7 @@ struct HeadLayout {
     int64_t piece = 0;       // columns of a piece of the vocabulary (a multiple of kHeadRows)
     int64_t pieces = 0;
     int64_t parts = 0;       // partial sums per token of the forward call
-    size_t index = 0;        // int32 [rows]: token of a row; rows are the tokens that count, in order
-    size_t place = 0;        // int32 [tokens]: row of a token, or -1
+    size_t place = 0;        // int32 [tokens]: row of a token, or -1; rows are the tokens that count, in order
     size_t target = 0;       // int32 [rows]: -1 where the target is outside the vocabulary
     size_t lse = 0;          // float [rows]
     size_t factor = 0;       // float [rows]: dloss

@@ -44,122 +44,158 @@ __device__ __forceinline__ float lifted(float z, float from)
     else return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, __builtin_fmaf(-from, kLog2e, float(kLift))));
 }
 
-// ---------------------------------------------------------------- which tokens count
+// ---------------------------------------------------------------- the tokens that count, and rows into place
 
-// One block lists the tokens that count, in order, with their targets and factors.  A token takes part if its target is not
-// `ignore` and (gradient) its factor is not 0; the products then run over that list alone.
-// Batches of 8192 tokens: eight loads in flight per thread, a count per wave and load by vote, a prefix sum over the 128 of them.
+// The tokens that count are listed, in order, with their targets and factors, and their hidden states copied into rows of whole steps.
+// A token takes part if its target is not `ignore` and (gradient) its factor is not 0; the products then run over that list alone.
+//
+// One launch does both: every block looks at all targets (a few loads per thread for some thousand tokens, against a launch's 3 us) for the
+// number of tokens that count, of those ahead of its own, and the largest factor; then it lists and copies its own.  Blocks past the
+// first list_blocks pad rows of the weight meanwhile, where these have to be (see HeadLayout::padded).
 constexpr int kListThreads = 1024, kListWaves = kListThreads / 64, kListEach = 8;
 
-__global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__restrict__ targets, const float *__restrict__ dloss,
-                                                            const float *__restrict__ lse_in, int64_t tokens, int64_t ignore,
-                                                            int64_t vocab, int32_t top_bits, Header *header,
-                                                            int32_t *__restrict__ index, int32_t *__restrict__ place,
-                                                            int32_t *__restrict__ target, float *__restrict__ lse,
-                                                            float *__restrict__ factor)
-{
-    __shared__ int32_t before[kListEach * kListWaves + 1];
-    __shared__ float tops[kListWaves];
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-    int32_t done = 0;
-    float top = 0.f;
-    for (int64_t first = 0; first < tokens; first += kListThreads * kListEach) {
-        int64_t v[kListEach];
-        float g[kListEach], l[kListEach];
-        uint64_t counts[kListEach];
-#pragma unroll
-        for (int k = 0; k < kListEach; k++) {
-            const int64_t t = first + k * kListThreads + tid;
-            v[k] = t < tokens ? targets[t] : ignore;
-            g[k] = dloss && t < tokens ? dloss[t] : 1.f;
-            l[k] = dloss && t < tokens ? lse_in[t] : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < kListEach; k++) {
-            const bool in = v[k] != ignore && g[k] != 0.f;
-            counts[k] = __ballot(in);
-            if (in) top = fmaxf(top, fabsf(g[k]));
-            if (lane == 0) before[k * kListWaves + wave] = __popcll(counts[k]);
-        }
-        __syncthreads();
-        if (wave == 0) {
-            const int32_t a = before[2 * lane], b = before[2 * lane + 1];
-            int32_t sum = a + b;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int32_t other = __shfl_up(sum, d, 64);
-                if (lane >= d) sum += other;
-            }
-            before[2 * lane] = sum - a - b;
-            before[2 * lane + 1] = sum - b;
-            if (lane == 63) before[kListEach * kListWaves] = sum;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kListEach; k++) {
-            const int64_t t = first + k * kListThreads + tid;
-            if (t >= tokens) continue;
-            if (!(counts[k] >> lane & 1)) {
-                place[t] = -1;
-                continue;
-            }
-            const int32_t row = done + before[k * kListWaves + wave] + __popcll(counts[k] & ((uint64_t(1) << lane) - 1));
-            const bool outside = v[k] < 0 || v[k] >= vocab;
-            index[row] = int32_t(t);
-            place[t] = row;
-            target[row] = outside ? -1 : int32_t(v[k]);
-            if (dloss) {
-                lse[row] = l[k];
-                factor[row] = outside ? __builtin_nanf("") : g[k];
-            }
-        }
-        done += before[kListEach * kListWaves];
-        __syncthreads();
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-    if (tid != 0) return;
-    for (int w = 0; w < kListWaves; w++) top = fmaxf(top, tops[w]);
-    // d is held under a power of two that moves the largest factor to [2^top_bits, 2^(top_bits + 1)): in binary16, with 14,
-    // probabilities down to 1e-9 stay normal numbers and nothing overflows, whatever the loss scale
-    int shift = 0;
-    if (top_bits && top > 0.f && top < __builtin_inff()) {
-        shift = top_bits - ilogbf(top);
-        shift = shift > 120 ? 120 : shift < -120 ? -120 : shift;
-    }
-    *header = Header{done, ldexpf(1.f, shift - (top_bits ? kLift : 0)), ldexpf(1.f, -shift)};
-}
-
-// ---------------------------------------------------------------- rows into place
-
-// A block per row: dst[row][0 .. pitch) = src[index ? index[row] : row][0 .. width), then zeros.  With a header, rows past the
-// count are zeros up to a whole step of the products' summed axis, and not written beyond.
+struct Lists {
+    int32_t *place, *target;
+    float *base, *factor;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void copy_rows(const T *__restrict__ src, int64_t width, T *__restrict__ dst, int64_t pitch,
-                                                 const Header *header, const int32_t *__restrict__ index, int32_t depth, int32_t in_place)
+struct Padding {
+    const T *src;
+    T *dst;
+    int64_t rows, width, pitch;
+};
+
+// A row of `width` elements, or (src null) of zeros, into a row of `pitch`, by `threads` threads.
+template <typename T>
+__device__ __forceinline__ void copy_row(const T *src, int64_t width, T *dst, int64_t pitch, int thread, int threads)
 {
     constexpr int kPer = 16 / int(sizeof(T));
     typedef uint32_t Vec __attribute__((ext_vector_type(4)));
-    int64_t row = blockIdx.x, from = row;
-    if (header) {
-        const int64_t count = header->count;
-        // the products read the hidden states themselves, see hidden_of
-        if (in_place && count == gridDim.x) return;
-        if (row >= (count + depth - 1) / depth * depth) return;
-        from = row < count ? index[row] : -1;
-    }
-    const T *s = src + from * width;
-    T *d = dst + row * pitch;
-    if (from < 0) {
-        for (int64_t k = int64_t(threadIdx.x) * kPer; k < pitch; k += 256 * kPer) *reinterpret_cast<Vec *>(d + k) = Vec{0, 0, 0, 0};
-    } else if (width % kPer == 0) {
-        for (int64_t k = int64_t(threadIdx.x) * kPer; k < pitch; k += 256 * kPer)
-            *reinterpret_cast<Vec *>(d + k) = k < width ? *reinterpret_cast<const Vec *>(s + k) : Vec{0, 0, 0, 0};
+    if (!src || width % kPer == 0) {
+        for (int64_t k = int64_t(thread) * kPer; k < pitch; k += int64_t(threads) * kPer)
+            *reinterpret_cast<Vec *>(dst + k) = src && k < width ? *reinterpret_cast<const Vec *>(src + k) : Vec{0, 0, 0, 0};
     } else {
-        for (int64_t k = int64_t(threadIdx.x); k < pitch; k += 256) d[k] = k < width ? s[k] : T(0.f);
+        for (int64_t k = thread; k < pitch; k += threads) dst[k] = k < width ? src[k] : T(0.f);
     }
+}
+
+// Sums of a pair of counts and the maximum of a value over a block, in every thread.
+struct Totals {
+    int32_t before, all;
+    float top;
+};
+__device__ __forceinline__ Totals block_totals(Totals t, Totals *waves)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        t.before += __shfl_xor(t.before, d, 64);
+        t.all += __shfl_xor(t.all, d, 64);
+        t.top = fmaxf(t.top, __shfl_xor(t.top, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = t;
+    __syncthreads();
+    t = waves[0];
+#pragma unroll
+    for (int w = 1; w < kListWaves; w++) {
+        t.before += waves[w].before;
+        t.all += waves[w].all;
+        t.top = fmaxf(t.top, waves[w].top);
+    }
+    return t;
+}
+
+// in_place: where every token counts, the products read the hidden states themselves (see Hidden) and nothing is copied.
+// depth: rows past the last one are zeros up to a whole step of the products' summed axis.
+template <typename T>
+__global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__restrict__ targets, const float *__restrict__ dloss,
+                                                            const float *__restrict__ lse, int64_t tokens, int64_t ignore, int64_t vocab,
+                                                            int32_t top_bits, const T *__restrict__ hidden, int64_t width, T *__restrict__ rows,
+                                                            int64_t pitch, int32_t depth, int32_t in_place, Header *header, Lists lists,
+                                                            uint32_t list_blocks, Padding<T> weight)
+{
+    __shared__ Totals totals[kListWaves];
+    __shared__ int32_t ahead[kListWaves], listed[kListThreads];
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+    if (blockIdx.x >= list_blocks) {
+        for (int64_t row = int64_t(blockIdx.x - list_blocks) * kListWaves + wave; row < weight.rows; row += int64_t(gridDim.x - list_blocks) * kListWaves)
+            copy_row(weight.src + row * weight.width, weight.width, weight.dst + row * weight.pitch, weight.pitch, lane, 64);
+        return;
+    }
+    const int64_t each = (tokens + list_blocks - 1) / list_blocks, first = int64_t(blockIdx.x) * each;
+    const int64_t end = first + each < tokens ? first + each : tokens;
+    const auto counts = [&](int64_t t) { return targets[t] != ignore && (!dloss || dloss[t] != 0.f); };
+    Totals mine{0, 0, 0.f};
+    for (int64_t from = 0; from < tokens; from += kListThreads * kListEach) {
+        int64_t v[kListEach];
+        float g[kListEach];
+#pragma unroll
+        for (int k = 0; k < kListEach; k++) {
+            const int64_t t = from + k * kListThreads + tid;
+            v[k] = t < tokens ? targets[t] : ignore;
+            g[k] = dloss && t < tokens ? dloss[t] : 1.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kListEach; k++) {
+            if (v[k] == ignore || g[k] == 0.f) continue;
+            mine.all++;
+            mine.before += from + k * kListThreads + tid < first;
+            mine.top = fmaxf(mine.top, fabsf(g[k]));
+        }
+    }
+    const Totals t = block_totals(mine, totals);
+    if (blockIdx.x == 0 && tid == 0) {
+        // d is held under a power of two that moves the largest factor to [2^top_bits, 2^(top_bits + 1)): in binary16, with 14,
+        // probabilities down to 1e-9 stay normal numbers and nothing overflows, whatever the loss scale
+        int shift = 0;
+        if (top_bits && t.top > 0.f && t.top < __builtin_inff()) {
+            shift = top_bits - ilogbf(t.top);
+            shift = shift > 120 ? 120 : shift < -120 ? -120 : shift;
+        }
+        *header = Header{t.all, ldexpf(1.f, shift - (top_bits ? kLift : 0)), ldexpf(1.f, -shift)};
+    }
+    const bool copies = !(in_place && t.all == tokens);
+    int32_t done = t.before;
+    for (int64_t from = first; from < end; from += kListThreads) {
+        const int64_t at = from + tid;
+        const bool in = at < end && counts(at);
+        const uint64_t vote = __ballot(in);
+        if (lane == 0) ahead[wave] = __popcll(vote);
+        __syncthreads();
+        int32_t before = __popcll(vote & ((uint64_t(1) << lane) - 1)), here = 0;
+        for (int w = 0; w < kListWaves; w++) {
+            before += w < wave ? ahead[w] : 0;
+            here += ahead[w];
+        }
+        if (at < end) {
+            const int32_t row = done + before;
+            lists.place[at] = in ? row : -1;
+            if (in) {
+                const int64_t v = targets[at];
+                const bool outside = v < 0 || v >= vocab;
+                listed[before] = int32_t(at - from);
+                lists.target[row] = outside ? -1 : int32_t(v);
+                if (dloss) {
+                    lists.base[row] = lse[at];
+                    lists.factor[row] = outside ? __builtin_nanf("") : dloss[at];
+                }
+            }
+        }
+        __syncthreads();
+        if (copies)
+            for (int32_t k = wave; k < here; k += kListWaves)
+                copy_row(hidden + (from + listed[k]) * width, width, rows + int64_t(done + k) * pitch, pitch, lane, 64);
+        done += here;
+    }
+    if (copies && blockIdx.x == list_blocks - 1)
+        for (int64_t row = done + wave; row < (int64_t(done) + depth - 1) / depth * depth; row += kListWaves)
+            copy_row(static_cast<const T *>(nullptr), width, rows + row * pitch, pitch, lane, 64);
+}
+
+// The weight in rows of whole steps; a block per row.
+template <typename T>
+__global__ __launch_bounds__(256) void pad_rows(const T *__restrict__ src, int64_t width, T *__restrict__ dst, int64_t pitch)
+{
+    copy_row(src + int64_t(blockIdx.x) * width, width, dst + int64_t(blockIdx.x) * pitch, pitch, int(threadIdx.x), 256);
 }
 
 // The hidden states that the products read: the caller's where every token counts and their rows fit the tiles as they are.
@@ -171,6 +207,23 @@ struct Hidden {
     __device__ __forceinline__ const T *of(int64_t count) const { return own && count == tokens ? own : listed; }
 };
 
+// The tokens of a loss call: listed, or as they come.  Few tokens are one row of tiles whether all of them count or not, and need no list
+// (a launch of 6 us beside 18 us for one token's logits); those that do not count get a loss of 0 in the end.
+struct Tokens {
+    const Header *header;    // null: as they come
+    const int32_t *place, *target;
+    const int64_t *targets;
+    int64_t tokens, ignore, vocab;
+    __device__ __forceinline__ int64_t count() const { return header ? header->count : tokens; }
+    __device__ __forceinline__ int32_t row_of(int64_t token) const { return header ? place[token] : targets[token] == ignore ? -1 : int32_t(token); }
+    __device__ __forceinline__ int32_t target_of(int64_t row) const
+    {
+        if (header) return target[row];
+        const int64_t v = targets[row];
+        return v < 0 || v >= vocab ? -1 : int32_t(v);
+    }
+};
+
 // ---------------------------------------------------------------- logits
 
 __device__ __forceinline__ uint32_t up(int64_t v, int to) { return uint32_t((v + to - 1) / to); }
@@ -180,14 +233,13 @@ using Lds = unsigned char[K::kLds];
 
 // Logits of a tile, and what its rows add to their softmax: the largest logit, the sum of exp(logit - it).
 template <typename K>
-__global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
+__global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                           int64_t pitch, int64_t first, int64_t columns, int64_t parts,
-                                                          const int32_t *__restrict__ target, float2 *__restrict__ stats,
-                                                          float *__restrict__ picked)
+                                                          float2 *__restrict__ stats, float *__restrict__ picked)
 {
     using T = typename K::T;
     __shared__ __align__(256) Lds<K> lds;
-    const int64_t count = header->count;
+    const int64_t count = tokens.count();
     int tm, tn;
     if (!tile_of_block(blockIdx.x, ~0u, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
@@ -208,7 +260,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
         const int m = tile.wm + 16 * i + r;
         const int64_t row = m0 + m;
         if (row < count) {
-            const int64_t d = int64_t(target[row]) - first - c0;
+            const int64_t d = int64_t(tokens.target_of(row)) - first - c0;
             if (d >= 0 && d < 16) {
 #pragma unroll
                 for (int j = 0; j < K::TN; j++)
@@ -252,14 +304,13 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(const Header *heade
 }
 
 // Joins the parts of every token's softmax: a wave per token.
-__global__ __launch_bounds__(256) void join_loss(int64_t tokens, int64_t parts, int64_t pitch, const int32_t *__restrict__ place,
-                                                 const int32_t *__restrict__ target, const float2 *__restrict__ stats,
+__global__ __launch_bounds__(256) void join_loss(Tokens tokens, int64_t parts, int64_t pitch, const float2 *__restrict__ stats,
                                                  const float *__restrict__ picked, float *__restrict__ loss, float *__restrict__ lse)
 {
     const int lane = int(threadIdx.x) & 63;
     const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (token >= tokens) return;
-    const int32_t row = place[token];
+    if (token >= tokens.tokens) return;
+    const int32_t row = tokens.row_of(token);
     if (row < 0) {
         if (lane == 0) loss[token] = lse[token] = 0.f;
         return;
@@ -292,7 +343,7 @@ __global__ __launch_bounds__(256) void join_loss(int64_t tokens, int64_t parts, 
     if (lane != 0) return;
     const float total = from + logf(sum);
     lse[token] = total;
-    loss[token] = target[row] < 0 ? __builtin_nanf("") : total - picked[row];
+    loss[token] = tokens.target_of(row) < 0 ? __builtin_nanf("") : total - picked[row];
 }
 
 // ---------------------------------------------------------------- gradient
@@ -592,27 +643,29 @@ struct Calls {
         const bool fits = !l.padded && l.tokens % head_depth(l.dt) == 0;
         return Hidden<T>{fits ? static_cast<const T *>(b.hidden) : nullptr, at<T>(l.hidden), l.tokens};
     }
+    // The list, and the first piece of the weight in padded rows where they have to be.
     void list(const float *dloss, const float *lse) const
     {
-        list_tokens<<<1, kListThreads, 0, stream>>>(b.targets, dloss, lse, l.tokens, b.ignore, l.vocab,
-                                                    l.dt == CGX_F16 ? 14 : l.dt == CGX_BF16 ? kLift : 0, header(), at<int32_t>(l.index), at<int32_t>(l.place),
-                                                    at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor));
-        launched();
         const Hidden<T> h = hidden();
-        const int64_t depth = head_depth(l.dt), rows = (l.tokens + depth - 1) / depth * depth;
-        if (rows) {
-            copy_rows<T><<<dim3(uint32_t(rows)), 256, 0, stream>>>(static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, header(),
-                                                                at<int32_t>(l.index), int32_t(depth), h.own ? 1 : 0);
-            launched();
-        }
+        const int64_t n = (l.tokens + 15) / 16, grid = n < 1 ? 1 : n < kHeadBlocks ? n : kHeadBlocks;
+        const int64_t columns = l.padded && l.tokens ? l.columns(0) : 0, wanted = (columns + kListThreads / 64 - 1) / (kListThreads / 64);
+        const int64_t pads = wanted < 8 * kHeadBlocks ? wanted : 8 * kHeadBlocks;
+        list_tokens<T><<<dim3(uint32_t(grid + pads)), kListThreads, 0, stream>>>(
+            b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, l.dt == CGX_F16 ? 14 : l.dt == CGX_BF16 ? kLift : 0,
+            static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, int32_t(head_depth(l.dt)), h.own ? 1 : 0, header(),
+            Lists{at<int32_t>(l.place), at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor)}, uint32_t(grid),
+            Padding<T>{static_cast<const T *>(b.weight), at<T>(l.weight), columns, l.width, l.pitch});
+        launched();
     }
-    // Rows `first` on of the weight, as the products read them.
+    // Rows `first` on of the weight, as the products read them.  (list() has padded the first piece.)
     const T *weight(int64_t first, int64_t columns) const
     {
         const T *w = static_cast<const T *>(b.weight) + first * l.width;
         if (!l.padded) return w;
-        copy_rows<T><<<dim3(uint32_t(columns)), 256, 0, stream>>>(w, l.width, at<T>(l.weight), l.pitch, nullptr, nullptr, 0, 0);
-        launched();
+        if (first > 0) {
+            pad_rows<T><<<dim3(uint32_t(columns)), 256, 0, stream>>>(w, l.width, at<T>(l.weight), l.pitch);
+            launched();
+        }
         return at<T>(l.weight);
     }
 
@@ -620,13 +673,18 @@ struct Calls {
     void loss_piece(int64_t first, int64_t columns) const
     {
         loss_tiles<K><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
-            header(), hidden(), weight(first, columns), l.pitch, first, columns, l.parts, at<int32_t>(l.target), at<float2>(l.stats),
-            at<float>(l.picked));
+            tokens(), direct() ? Hidden<T>{static_cast<const T *>(b.hidden), nullptr, l.tokens} : hidden(), weight(first, columns), l.pitch,
+            first, columns, l.parts, at<float2>(l.stats), at<float>(l.picked));
         launched();
+    }
+    bool direct() const { return l.tokens <= 64 && !l.padded; }
+    Tokens tokens() const
+    {
+        return Tokens{direct() ? nullptr : header(), at<int32_t>(l.place), at<int32_t>(l.target), b.targets, l.tokens, b.ignore, l.vocab};
     }
     hipError_t loss(float *loss, float *lse) const
     {
-        list(nullptr, nullptr);
+        if (!direct()) list(nullptr, nullptr);
         // (a weight that needs no padding is walked in one launch)
         const int64_t piece = l.padded ? l.piece : l.vocab;
         const Size size = size_of<T>(l.tokens, piece);
@@ -637,9 +695,8 @@ struct Calls {
             else loss_piece<Tiny<T, kSumContiguous, kSumStrips>>(first, columns);
         }
         const int side = size == kLarge ? 256 : size == kSmall ? 128 : 64;
-        join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(l.tokens, (l.vocab + side - 1) / side, l.parts, at<int32_t>(l.place),
-                                                                      at<int32_t>(l.target), at<float2>(l.stats), at<float>(l.picked), loss,
-                                                                      lse);
+        join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(tokens(), (l.vocab + side - 1) / side, l.parts, at<float2>(l.stats),
+                                                                      at<float>(l.picked), loss, lse);
         launched();
         return error;
     }
@@ -684,8 +741,9 @@ struct Calls {
     hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight) const
     {
         list(dloss, lse);
-        // (sums over the vocabulary are split where they have few tiles: tiles of few tokens' rows need only be no larger than these)
-        const bool wide = l.tokens > 64;
+        // (sums over the vocabulary are split where they have few tiles: only where no split fills the chip the tiles have to be tiny)
+        using Wide = Large<T, kSumContiguous, kRowContiguous>;
+        const bool wide = l.tokens > 64 && tiles(l.tokens, l.pitch, Wide::BM) * (l.piece / (kLeastSteps * Wide::kDepth)) >= 192;
         for (int64_t k = 0; k < l.pieces; k++) {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
