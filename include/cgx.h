@@ -448,7 +448,7 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  *              of them
  *   workspace  device, 16-byte aligned, at least the bytes cgx_grad_norm_workspace reports (CGX_ERR_SIZE
  *              otherwise).  Calls that share one must not overlap.
- * A launch covers up to 160 tensors; longer lists take more.
+ * A launch covers up to 240 tensors; longer lists take more.
  */
 typedef struct {
     void *data;       /* device */
