@@ -407,11 +407,26 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
 
 // Into how many parts the sum over a piece is split, so that the tiles of few tokens fill the chip too: as many as `blocks` allow,
 // of at least kLeastSteps steps.  Each part has sums of its own, joined by round_hidden in order.
-constexpr int kLeastSteps = 4;
+constexpr int kLeastSteps = 8;
 __device__ __forceinline__ uint32_t parts_of(uint32_t tiles, uint32_t steps, uint32_t blocks)
 {
     const uint32_t most = steps / kLeastSteps, parts = tiles ? blocks / tiles : 1;
     return parts < 1 || most < 1 ? 1 : parts < most ? parts : most;
+}
+
+// The sum of the parts, in order, with eight of them on their way at a time.
+__device__ __forceinline__ f32x4 joined(const float *first, int64_t apart, uint32_t parts)
+{
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t p = 0; p < parts; p += 8) {
+        f32x4 x[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; k++)
+            x[k] = p + k < parts ? *reinterpret_cast<const f32x4 *>(first + int64_t(p + k) * apart) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (uint32_t k = 0; k < 8; k++) v += x[k];
+    }
+    return v;
 }
 
 // dx += d W over a piece.  accumulate: not the first piece.
@@ -556,9 +571,7 @@ __global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t
         const int m = int(strip) * kStrip + k / K::BN, n = k % K::BN;
         const int64_t row = int64_t(tm) * K::BM + m, column = int64_t(tn) * K::BN + n;
         if (row >= columns || column >= width) continue;
-        f32x4 v{0.f, 0.f, 0.f, 0.f};
-        for (uint32_t p = 0; p < r.parts; p++)
-            v += *reinterpret_cast<const f32x4 *>(spare + (int64_t(p) * r.rest + at) * (K::BM * K::BN) + m * K::BN + n);
+        const f32x4 v = joined(spare + int64_t(at) * (K::BM * K::BN) + m * K::BN + n, int64_t(r.rest) * (K::BM * K::BN), r.parts);
         store_weights(dweight, row, column, width, v, unscale);
     }
 }
@@ -577,9 +590,7 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
     const float *s = sums + int64_t(row < 0 ? 0 : row) * pitch;
     T *d = dhidden + token * width;
     for (int64_t k = int64_t(threadIdx.x) * 4; k < width; k += 1024) {
-        f32x4 v{0.f, 0.f, 0.f, 0.f};
-        if (row >= 0)
-            for (uint32_t p = 0; p < parts; p++) v += *reinterpret_cast<const f32x4 *>(s + int64_t(p) * count * pitch + k);
+        const f32x4 v = row < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : joined(s + k, count * pitch, parts);
         Four out;
 #pragma unroll
         for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
@@ -596,23 +607,35 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
 // ---------------------------------------------------------------- launches
 
 // Three tiles.  The large one reads each operand least often; the smaller ones fill the chip's 256 compute units (one, two and four blocks
-// each) where there are few of it, or where the tokens do not fill its rows.
+// each) where there are few of it, or where the tokens do not fill its rows.  Binary32 products are bound by the matrix cores, which the
+// tiny tile keeps as busy as the others, with more of it in flight and less lost in the last round: us with small and with tiny tiles,
+// 300 x 2048 x 30000 with gradients 1450 and 1309, 2000 x 1500 x 5000 1133 and 1048, the loss of 509 x 768 x 30522 200 and 192.
 template <typename T, Layout LA, Layout LB>
 using Tiny = Tile<T, 64, 64, 4, 1, LA, LB>;
 template <typename T, Layout LA, Layout LB>
-using Small = Tile<T, 128, 128, 2, 2, LA, LB>;
-// (binary32 products are bound by the matrix cores, which the small tile keeps as busy)
+using Small = std::conditional_t<sizeof(T) == 2, Tile<T, 128, 128, 2, 2, LA, LB>, Tiny<T, LA, LB>>;
 template <typename T, Layout LA, Layout LB>
-using Large = std::conditional_t<sizeof(T) == 2, Tile<T, 256, 256, 2, 4, LA, LB>, Small<T, LA, LB>>;
+using Large = std::conditional_t<sizeof(T) == 2, Tile<T, 256, 256, 2, 4, LA, LB>, Tiny<T, LA, LB>>;
 
 int64_t tiles(int64_t rows, int64_t columns, int side) { return ((rows + side - 1) / side) * ((columns + side - 1) / side); }
 
 enum Size { kTiny, kSmall, kLarge };
+
+// Which tile a product of rows x columns takes: the one with the least time, in rounds of the large one, of which the others do 0.91 and
+// 0.6 of the work.  split: steps of a summed axis over which a last, partial round may be split (weight_tiles), which costs a pass over
+// its parts.  Measured, us with large and with small tiles for the weight's gradient: 1500 tokens x 768 x 30522 349 and 332 (1.4 rounds),
+// 2048 x 1024 x 50257 840 and 889 (3.1 rounds, split); for the loss of 2048 x 2048 x 50257 353 and 375 (6.2 and 12.3 rounds).
 template <typename T>
-Size size_of(int64_t rows, int64_t columns)
+Size size_of(int64_t rows, int64_t columns, int64_t split = 0)
 {
-    if (sizeof(T) == 2 && rows > 128 && tiles(rows, columns, 256) >= 192) return kLarge;
-    return rows > 64 && tiles(rows, columns, 128) >= 192 ? kSmall : kTiny;
+    if (sizeof(T) == 4) return kTiny;
+    const auto rounds = [&](int side, int64_t blocks) {
+        const int64_t n = tiles(rows, columns, side), rest = n % blocks, most = split / kLeastSteps;
+        const int64_t parts = rest && blocks / rest < most ? blocks / rest : most;
+        return double(n / blocks) + (!rest ? 0.0 : parts >= 2 ? 1.0 / double(parts) + 0.16 : 1.0);
+    };
+    const double large = rounds(256, kHeadBlocks), small = rounds(128, 2 * kHeadBlocks) * 0.5 / 0.91, tiny = rounds(64, 4 * kHeadBlocks) * 0.25 / 0.6;
+    return large <= small && large <= tiny ? kLarge : small <= tiny ? kSmall : kTiny;
 }
 
 template <typename T>
@@ -743,7 +766,7 @@ struct Calls {
         list(dloss, lse);
         // (sums over the vocabulary are split where they have few tiles: only where no split fills the chip the tiles have to be tiny)
         using Wide = Large<T, kSumContiguous, kRowContiguous>;
-        const bool wide = l.tokens > 64 && tiles(l.tokens, l.pitch, Wide::BM) * (l.piece / (kLeastSteps * Wide::kDepth)) >= 192;
+        const bool wide = sizeof(T) == 2 && l.tokens > 64 && tiles(l.tokens, l.pitch, Wide::BM) * (l.piece / (kLeastSteps * Wide::kDepth)) >= 192;
         for (int64_t k = 0; k < l.pieces; k++) {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
@@ -755,7 +778,7 @@ struct Calls {
                 if (wide) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
                 else hidden_sums<Tiny<T, kSumContiguous, kRowContiguous>>(w, first, columns);
             }
-            const Size size = size_of<T>(columns, l.width);
+            const Size size = size_of<T>(columns, l.width, (l.tokens + head_depth(l.dt) - 1) / head_depth(l.dt));
             if (size == kLarge) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
             else if (size == kSmall) weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
             else weight_rows<Tiny<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
