@@ -406,8 +406,8 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
  *   d[n][v]       = dloss[n] * (exp(z[n][v] - lse[n]) - (v == targets[n]))
  *   dhidden[n][h] = sum_v d[n][v] * weight[v][h],  dweight[v][h] = sum_n d[n][v] * hidden[n][h]
  * Logits are formed tile by tile and kept by neither call; the second one forms them again, holds d for a
- * piece of the vocabulary at a time in the workspace, and in the type of the operands (for binary16 under
- * a power of two that keeps it in range).  Products are summed in binary32, each result is rounded once.
+ * piece of the vocabulary at a time in the workspace, in the type of the operands (16-bit types: in units of
+ * the largest dloss, which keeps it in range).  Products are summed in binary32, each result is rounded once.
  * The order of every sum is fixed: the same call gives the same bits again.
  *   hidden    device, tokens x width elements of dt (CGX_F32, CGX_F16 or CGX_BF16), dense
  *   weight    device, vocab x width elements of dt, dense

@@ -29,7 +29,7 @@ struct HeadLayout {
     size_t place = 0;        // int32 [tokens]: row of a token, or -1; rows are the tokens that count, in order
     size_t target = 0;       // int32 [rows]: -1 where the target is outside the vocabulary
     size_t lse = 0;          // float [rows]
-    size_t factor = 0;       // float [rows]: dloss
+    size_t factor = 0;       // float [rows]: dloss in the units of d
     size_t picked = 0;       // float [rows]: the target's logit
     size_t hidden = 0;       // T [rows][pitch]
     size_t weight = 0;       // T [piece][pitch], where padded

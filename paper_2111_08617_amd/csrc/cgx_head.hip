@@ -19,11 +19,11 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Header {
     int32_t count;           // tokens that count
-    float scale, unscale;    // powers of two: what lifted probabilities are multiplied by to give d, and the products of d
+    float unscale;           // what the products of d are multiplied by
 };
 
 // The hardware's exp2 gives 0 below 2^-126; d of 16-bit types is formed from probabilities lifted by this much, which keeps those
-// down to 2^-150, and its scale takes the lift out again.
+// down to 2^-150, and the units of its factor take the lift out again.
 constexpr int kLift = 24;
 template <typename T>
 constexpr int lift_of = sizeof(T) == 2 ? kLift : 0;
@@ -143,16 +143,12 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
         }
     }
     const Totals t = block_totals(mine, totals);
-    if (blockIdx.x == 0 && tid == 0) {
-        // d is held under a power of two that moves the largest factor to [2^top_bits, 2^(top_bits + 1)): in binary16, with 14,
-        // probabilities down to 1e-9 stay normal numbers and nothing overflows, whatever the loss scale
-        int shift = 0;
-        if (top_bits && t.top > 0.f && t.top < __builtin_inff()) {
-            shift = top_bits - ilogbf(t.top);
-            shift = shift > 120 ? 120 : shift < -120 ? -120 : shift;
-        }
-        *header = Header{t.all, ldexpf(1.f, shift - (top_bits ? kLift : 0)), ldexpf(1.f, -shift)};
-    }
+    // d is held in units of the largest factor, times 2^top_bits.  With factors that are all alike (a mean over tokens) a target that has
+    // no probability yet then is exactly -2^top_bits, and near 1 the rounding is at its finest: in units of 1 all targets of a call
+    // would be off by the same rounding of the factor, and with them the whole gradient, by up to 2^-8.  In binary16, with 14, probabilities down to
+    // 1e-9 stay normal numbers and nothing overflows, whatever the loss scale.
+    const float unit = !top_bits || !(t.top < __builtin_inff()) || t.top == 0.f ? 1.f : fmaxf(t.top, 0x1p-100f);
+    if (blockIdx.x == 0 && tid == 0) *header = Header{t.all, ldexpf(unit, -top_bits)};
     const bool copies = !(in_place && t.all == tokens);
     int32_t done = t.before;
     for (int64_t from = first; from < end; from += kListThreads) {
@@ -176,7 +172,7 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
                 lists.target[row] = outside ? -1 : int32_t(v);
                 if (dloss) {
                     lists.base[row] = lse[at];
-                    lists.factor[row] = outside ? __builtin_nanf("") : dloss[at];
+                    lists.factor[row] = outside ? __builtin_nanf("") : top_bits ? ldexpf(dloss[at] / unit, top_bits - kLift) : dloss[at];
                 }
             }
         }
@@ -348,7 +344,7 @@ __global__ __launch_bounds__(256) void join_loss(Tokens tokens, int64_t parts, i
 
 // ---------------------------------------------------------------- gradient
 
-// d of a tile of a piece: logits as above, then dloss (exp(z - lse) - [v = target]) under the scale, in the operands' type.
+// d of a tile of a piece: logits as above, then dloss (exp(z - lse) - [v = target]) in its units, in the operands' type.
 // Every element of the piece's whole tiles is written; those of no token or no column are zeros.
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
@@ -359,7 +355,6 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     using T = typename K::T;
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
-    const float scale = header->scale;
     int tm, tn;
     if (!tile_of_block(blockIdx.x, ~0u, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
@@ -381,7 +376,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
         const bool counts = row < count;
-        const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] * scale : 0.f;
+        const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] : 0.f;
         const int64_t hit = counts ? int64_t(target[row]) - first - c0 : -1;
         T *const out = delta + row * piece + c0;
 #pragma unroll
