@@ -201,3 +201,22 @@ def test_streams_and_graphs(torch):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(norm, want[0]) and torch.equal(fused, want[1])
+
+
+@pytest.mark.parametrize("odd", [False, True])
+def test_lengths_around_an_items_and_lists_around_a_launchs(torch, odd):
+    """Items of 4096 elements, 240 tensors a launch, results above and below the size from which they are streamed."""
+    for sizes in ([4095, 4096, 4097, 0, 8191, 1], [3] * 239, [3] * 240, [3] * 241, [2] * 480 + [0] * 5 + [7], [1 << 25, 4097, 3 << 22]):
+        grads = tensors(torch, sizes, ("bf16", "f32", "f16"), seed=len(sizes), odd=odd)
+        norm, total = norm_of(torch, grads), exact(grads)
+        assert abs(float(norm) - total) <= 2.0**-23 * total
+        max_norm = float(np.float32(total / 2))
+        want = torch.cat(expected(torch, grads, norm, max_norm, torch.float32))
+        fused = torch.full((sum(sizes) + 64,), -7.0, device="cuda")
+        cgx.cgx_grad_clip(grads, norm, max_norm, out=fused)
+        torch.cuda.synchronize()
+        assert same_bits(torch, fused[:sum(sizes)], want) and (fused[sum(sizes):] == -7.0).all()
+        in_place = expected(torch, grads, norm, max_norm)
+        cgx.cgx_grad_clip(grads, norm, max_norm)
+        torch.cuda.synchronize()
+        assert all(same_bits(torch, g, w) for g, w in zip(grads, in_place))

@@ -275,3 +275,22 @@ def test_the_last_round_of_the_weights_tiles(torch, tokens, dtype):
     hidden, weight, targets = inputs(torch, tokens, 1024, 16640 - 3, dtype, seed=tokens)
     targets[5::9] = -100
     check(torch, hidden, weight, targets, torch.full((tokens,), 1.0 / tokens, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens", [8, 30, 100, 1000])
+def test_a_means_factor_is_not_rounded_in_every_target(torch, tokens, dtype):
+    """1 / tokens is no number of 16 bits.  Were d rounded in units of 1, every target of a call would be off by the same 2^-9 (2^-12) or so,
+    and the gradients of tokens that a model knows nothing of with them.  A target at probability p is -(1 - p) in units of the factor:
+    stored as -1, off by p, where p is below half a unit roundoff (here about 1 / vocab); the other elements of d, each off by up to u of
+    itself and in no common direction, hold 1 / sqrt(vocab) of its size.  So a gradient is hardly further from the exact one than that one
+    rounded to its type."""
+    vocab, width = 20000, 256
+    hidden, weight, targets = inputs(torch, tokens, width, vocab, dtype, seed=17, size=0.05)
+    got = call(torch, hidden, weight, targets, torch.full((tokens,), 1.0 / tokens, device="cuda"))
+    x, w = hidden.double(), weight.double()
+    d = torch.softmax(torch.mm(x, w.t()), dim=1)
+    d[torch.arange(tokens, device="cuda"), targets] -= 1.0
+    for name, want in (("dhidden", torch.mm(d, w) / tokens), ("dweight", torch.mm(d.t().contiguous(), x) / tokens)):
+        off, rounded = (float((t.double() - want).norm() / want.norm()) for t in (got[name], want.to(hidden.dtype)))
+        assert off <= rounded + 2.0 / vocab + 0.05 * ROUNDOFF[dtype], (name, off, rounded)
