@@ -618,8 +618,9 @@ enum Size { kTiny, kSmall, kLarge };
 
 // Which tile a product of rows x columns takes: the one with the least time, in rounds of the large one, of which the others do 0.91 and
 // 0.6 of the work.  split: steps of a summed axis over which a last, partial round may be split (weight_tiles), which costs a pass over
-// its parts.  Measured, us with large and with small tiles for the weight's gradient: 1500 tokens x 768 x 30522 349 and 332 (1.4 rounds),
-// 2048 x 1024 x 50257 840 and 889 (3.1 rounds, split); for the loss of 2048 x 2048 x 50257 353 and 375 (6.2 and 12.3 rounds).
+// its parts in a launch of its own (of about three steps' time).  Measured, us with large and with small tiles for the weight's gradient:
+// 1500 tokens x 768 x 30522 349 and 332 (1.4 rounds), 2048 x 1024 x 50257 840 and 889 (3.1 rounds, split); for the loss of 2048 x 2048 x
+// 50257 353 and 375 (6.2 and 12.3 rounds).
 template <typename T>
 Size size_of(int64_t rows, int64_t columns, int64_t split = 0)
 {
@@ -627,7 +628,7 @@ Size size_of(int64_t rows, int64_t columns, int64_t split = 0)
     const auto rounds = [&](int side, int64_t blocks) {
         const int64_t n = tiles(rows, columns, side), rest = n % blocks, most = split / kLeastSteps;
         const int64_t parts = rest && blocks / rest < most ? blocks / rest : most;
-        return double(n / blocks) + (!rest ? 0.0 : parts >= 2 ? 1.0 / double(parts) + 0.16 : 1.0);
+        return double(n / blocks) + (!rest ? 0.0 : parts >= 2 ? 1.0 / double(parts) + 0.12 + 3.0 / double(split) : 1.0);
     };
     const double large = rounds(256, kHeadBlocks), small = rounds(128, 2 * kHeadBlocks) * 0.5 / 0.91, tiny = rounds(64, 4 * kHeadBlocks) * 0.25 / 0.6;
     return large <= small && large <= tiny ? kLarge : small <= tiny ? kSmall : kTiny;
@@ -727,6 +728,19 @@ struct Calls {
             l.piece);
         launched();
     }
+    // The tile of dx: its sum over the vocabulary is split where there are few of it, so that any size fills the chip, and each part is written
+    // and read again.  The larger tile, then, where it needs few parts.  Whole calls with large and with small tiles, us: 2048 x 1024 x 50257 (32
+    // large tiles) 846 and 896, 600 x 2048 x 50257 (24) 629 and 619, 1500 x 768 x 30522 (18) 346 and 344.
+    Size sums_size() const
+    {
+        if (sizeof(T) == 4 || l.tokens <= 64) return kTiny;
+        const auto blocks_of = [&](int side, int64_t most) {
+            const int64_t n = tiles(l.tokens, l.pitch, side), parts = l.piece / (kLeastSteps * head_depth(l.dt));
+            return n * (most / n < 1 ? 1 : most / n < parts ? most / n : parts);
+        };
+        if (tiles(l.tokens, l.pitch, 256) >= 32 && blocks_of(256, blocks<Large<T, kSumContiguous, kRowContiguous>>) >= 192) return kLarge;
+        return blocks_of(128, 2 * kHeadBlocks) >= 384 ? kSmall : kTiny;
+    }
     template <typename K>
     void hidden_sums(const T *w, int64_t first, int64_t columns) const
     {
@@ -759,9 +773,7 @@ struct Calls {
     hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight) const
     {
         list(dloss, lse);
-        // (sums over the vocabulary are split where they have few tiles: only where no split fills the chip the tiles have to be tiny)
-        using Wide = Large<T, kSumContiguous, kRowContiguous>;
-        const bool wide = sizeof(T) == 2 && l.tokens > 64 && tiles(l.tokens, l.pitch, Wide::BM) * (l.piece / (kLeastSteps * Wide::kDepth)) >= 192;
+        const Size sums = sums_size();
         for (int64_t k = 0; k < l.pieces; k++) {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
@@ -770,7 +782,8 @@ struct Calls {
                 if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                if (wide) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                if (sums == kLarge) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                else if (sums == kSmall) hidden_sums<Small<T, kSumContiguous, kRowContiguous>>(w, first, columns);
                 else hidden_sums<Tiny<T, kSumContiguous, kRowContiguous>>(w, first, columns);
             }
             const Size size = size_of<T>(columns, l.width, (l.tokens + head_depth(l.dt) - 1) / head_depth(l.dt));
@@ -778,8 +791,10 @@ struct Calls {
             else if (size == kSmall) weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
             else weight_rows<Tiny<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
         }
-        if (l.tokens && wide) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
-        else if (l.tokens) rounded<Tiny<T, kSumContiguous, kRowContiguous>>(dhidden);
+        if (!l.tokens) return error;
+        if (sums == kLarge) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
+        else if (sums == kSmall) rounded<Small<T, kSumContiguous, kRowContiguous>>(dhidden);
+        else rounded<Tiny<T, kSumContiguous, kRowContiguous>>(dhidden);
         return error;
     }
 };
