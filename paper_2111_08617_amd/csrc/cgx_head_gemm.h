@@ -61,6 +61,13 @@ __device__ __forceinline__ void to_lds(const void *base, uint32_t offset, uint32
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
 }
+// A barrier that no LDS access moves across (what it is a barrier for has been waited for by then: unlike __syncthreads, it adds no waits).
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
 __device__ __forceinline__ uint32_t lds_address(const void *p)
 {
     return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
@@ -232,7 +239,7 @@ struct Tile {
         if constexpr (NEXT) {
             // the next stage is here, and everybody is done reading this one
             wait_loads_and_reads();
-            __builtin_amdgcn_s_barrier();
+            barrier();
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (LOAD) {
                 a.load(at + now, wave);
@@ -272,7 +279,7 @@ struct Tile {
         a.load(at, wave);
         b.load(at + A::kBytes, wave);
         wait_loads_and_reads();
-        __builtin_amdgcn_s_barrier();
+        barrier();
         if (steps > 1) {
             if (steps == 2) shorten();
             a.load(at + kStage, wave);

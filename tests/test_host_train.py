@@ -168,3 +168,27 @@ def test_binding_refuses_what_the_kernels_would_overrun(lib):
         cgx.cgx_grad_clip(some, Fake((1,), f), 1.0, out=Fake((265,), torch.int64))
     with pytest.raises(ValueError, match="lives on|device"):
         cgx.cgx_grad_norm([torch.zeros(4)], Fake((1,), f), good["workspace"])
+
+
+def test_head_sizes_a_launch_cannot_hold(lib):
+    n = ctypes.c_size_t()
+    for tokens, width, vocab in ((1 << 20, 64, 1 << 16), (1 << 20, 1 << 16, 100), ((1 << 24) - 1, 1 << 17, 1)):
+        assert lib.cgx_head_workspace(tokens, width, vocab, 0, 1, ctypes.byref(n)) == SIZE
+    assert lib.cgx_head_workspace(1 << 20, 4096, 50257, 2, 1, ctypes.byref(n)) == OK
+    # pieces of the vocabulary stay small beside what a million tokens need themselves
+    assert n.value < 2 * ((1 << 20) * 4096 * (2 + 4)) + (4 << 30)
+
+
+def test_workspace_layout_is_clean_under_asan_and_ubsan(tmp_path):
+    """The host code that lays the workspace out, with a driver that checks every section's place on many sizes."""
+    import shutil
+    import subprocess
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "driver")
+    subprocess.run(["g++", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-g", "-O1", "-std=c++17",
+                    os.path.join(here, "host_sanitize", "head_layout.cpp"),
+                    os.path.join(os.path.dirname(here), "paper_2111_08617_amd", "csrc", "cgx_head.cpp"), "-o", exe], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "all checks passed" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
