@@ -11,6 +11,8 @@ namespace cgx {
 constexpr int kHeadRows = 256;                       // token rows and columns of a piece come in multiples of it (the largest tile)
 constexpr int kHeadBlocks = 256;                     // compute units: a sum is split into parts where its tiles are fewer
 constexpr size_t kHeadHeaderBytes = 256;
+constexpr int kFewTokens = 16;                       // up to this many, the loss has a kernel of its own, a block of it for
+constexpr int kFewColumns = 32;                      // this many columns of the vocabulary
 
 inline size_t head_element(int dt) { return dt == CGX_F32 ? 4 : 2; }
 // Elements of the summed axis per step of the products: rows are padded to a multiple of it.

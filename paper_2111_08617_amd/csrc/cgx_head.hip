@@ -71,11 +71,36 @@ __device__ __forceinline__ void copy_row(const T *src, int64_t width, T *dst, in
 {
     constexpr int kPer = 16 / int(sizeof(T));
     typedef uint32_t Vec __attribute__((ext_vector_type(4)));
+    // (eight loads on their way at a time)
+    constexpr int kAhead = 8;
     if (!src || width % kPer == 0) {
-        for (int64_t k = int64_t(thread) * kPer; k < pitch; k += int64_t(threads) * kPer)
-            *reinterpret_cast<Vec *>(dst + k) = src && k < width ? *reinterpret_cast<const Vec *>(src + k) : Vec{0, 0, 0, 0};
+        for (int64_t from = int64_t(thread) * kPer; from < pitch; from += int64_t(threads) * kPer * kAhead) {
+            Vec v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const int64_t k = from + int64_t(i) * threads * kPer;
+                v[i] = src && k < width ? *reinterpret_cast<const Vec *>(src + k) : Vec{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const int64_t k = from + int64_t(i) * threads * kPer;
+                if (k < pitch) *reinterpret_cast<Vec *>(dst + k) = v[i];
+            }
+        }
     } else {
-        for (int64_t k = thread; k < pitch; k += threads) dst[k] = k < width ? src[k] : T(0.f);
+        for (int64_t from = thread; from < pitch; from += int64_t(threads) * kAhead) {
+            T v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const int64_t k = from + int64_t(i) * threads;
+                v[i] = k < width ? src[k] : T(0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const int64_t k = from + int64_t(i) * threads;
+                if (k < pitch) dst[k] = v[i];
+            }
+        }
     }
 }
 
@@ -299,25 +324,123 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
     }
 }
 
-// Joins the parts of every token's softmax: a wave per token.
-__global__ __launch_bounds__(256) void join_loss(Tokens tokens, int64_t parts, int64_t pitch, const float2 *__restrict__ stats,
-                                                 const float *__restrict__ picked, float *__restrict__ loss, float *__restrict__ lse)
+// The same for up to 16 tokens, where reading W is all that takes time: a block per kFewColumns rows of W, whose four waves each sum a
+// quarter of the width.  W goes from memory to the registers of the one wave that uses it, a unit of 128 bytes per row ahead of the products,
+// so there are no barriers on the way and every wave has its own loads in flight; tokens are read from the caches, at half of W's bytes.
+// Calls with it and with tiny tiles, us: 1 x 2048 x 50257 bfloat16 (206 MB) 44 and 56, 1 x 4096 x 50257 82 and 96, 16 x 2048 x 50257 48 and 60,
+// 16 x 768 x 30522 binary32 28 and 38; 103 MB that the memory-side cache partly holds 23 and 22, that it does not 25 and 27.  For 32 and 64
+// tokens the same with two and four times the tokens per wave was slower than the tiles (206 MB 62 and 62, 84 and 62): tokens then cost as
+// many bytes of the caches as W or more.  32 columns a block: 16 and 64 took 59 and 51 instead of 49 for 16 x 2048 x 50257.
+constexpr int kFewWaves = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, const T *__restrict__ hidden, const T *__restrict__ weight,
+                                                               int64_t pitch, int64_t parts, float2 *__restrict__ stats,
+                                                               float *__restrict__ picked)
 {
-    const int lane = int(threadIdx.x) & 63;
-    const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (token >= tokens.tokens) return;
-    const int32_t row = tokens.row_of(token);
-    if (row < 0) {
-        if (lane == 0) loss[token] = lse[token] = 0.f;
+    using E = Element<T>;
+    using Frag = typename E::Frag;
+    constexpr int TN = kFewColumns / 16, kUnit = kStepBytes / int(sizeof(T)), kPitch = kFewColumns + 4;
+    __shared__ __align__(16) float part[kFewWaves][16][kPitch];
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
+    const int64_t n0 = int64_t(blockIdx.x) * kFewColumns;
+    const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens);
+    // (rows past the last one are read from it, and not used)
+    uint32_t of_column[TN];
+    const uint32_t of_token = uint32_t(r < count ? r : count - 1) * uint32_t(pitch * sizeof(T)) + g * 16;
+#pragma unroll
+    for (int j = 0; j < TN; j++) of_column[j] = uint32_t(16 * j + r < columns ? 16 * j + r : columns - 1) * uint32_t(pitch * sizeof(T)) + g * 16;
+    struct Unit {
+        Frag a[2], b[2][TN];
+    };
+    const int units = int(pitch / kUnit), from = units * wave / kFewWaves, to = units * (wave + 1) / kFewWaves;
+    const unsigned char *w = reinterpret_cast<const unsigned char *>(weight + n0 * pitch), *x = reinterpret_cast<const unsigned char *>(hidden);
+    const auto load = [&](Unit &u, int at) {
+#pragma unroll
+        for (int half = 0; half < 2; half++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) u.b[half][j] = *reinterpret_cast<const Frag *>(w + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_column[j]);
+#pragma unroll
+        for (int half = 0; half < 2; half++)
+            u.a[half] = *reinterpret_cast<const Frag *>(x + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_token);
+    };
+    f32x4 acc[TN];
+#pragma unroll
+    for (int j = 0; j < TN; j++) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto multiply = [&](const Unit &u) {
+#pragma unroll
+        for (int half = 0; half < 2; half++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) acc[j] = E::mfma(u.b[half][j], u.a[half], acc[j]);
+    };
+    if (from < to) {
+        Unit u0, u1;
+        load(u0, from);
+        int at = from;
+        for (; at + 2 < to; at += 2) {
+            load(u1, at + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u0);
+            __builtin_amdgcn_sched_barrier(0);
+            load(u0, at + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (at + 1 < to) load(u1, at + 1);
+        multiply(u0);
+        if (at + 1 < to) multiply(u1);
+    }
+#pragma unroll
+    for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(&part[wave][r][16 * j + 4 * g]) = acc[j];
+    __syncthreads();
+    // a token's columns: kLanes neighbouring lanes, kEach columns a lane
+    constexpr int kEach = 16 * kFewColumns / (64 * kFewWaves), kLanes = kFewColumns / kEach;
+    const int m = tid / kLanes, first = tid % kLanes * kEach;
+    const int32_t target = m < count ? tokens.target_of(m) : -1;
+    float z[kEach], top = -__builtin_inff();
+#pragma unroll
+    for (int e = 0; e < kEach; e++) {
+        z[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; k++) z[e] += part[k][m][first + e];
+        if (m < count && target == n0 + first + e) picked[m] = z[e];
+        if (first + e >= columns) z[e] = -__builtin_inff();
+        top = fmaxf(top, z[e]);
+    }
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kEach; e++) sum += exp_from<T>(z[e], base);
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if (m < count && first == 0) stats[m * parts + blockIdx.x] = float2{top, sum};
+}
+
+// Joins the parts of every token's softmax: a wave per token, four of them in a block, or (few tokens) a block of many waves per token.
+constexpr int kJoinWaves = 16;
+template <int WAVES>
+constexpr int join_tokens = WAVES > 1 ? 1 : 4;
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tokens tokens, int64_t parts, int64_t pitch, const float2 *__restrict__ stats,
+                                                             const float *__restrict__ picked, float *__restrict__ loss, float *__restrict__ lse)
+{
+    constexpr int kLanes = 64 * WAVES;
+    const int lane = int(threadIdx.x) % kLanes;
+    const int64_t token = int64_t(blockIdx.x) * join_tokens<WAVES> + threadIdx.x / kLanes;
+    const int32_t row = token < tokens.tokens ? tokens.row_of(token) : -1;
+    if (row < 0) {                                       // (for WAVES > 1, the whole block's row)
+        if (token < tokens.tokens && lane == 0) loss[token] = lse[token] = 0.f;
         return;
     }
     const float2 *s = stats + row * pitch;
     float top = -__builtin_inff(), sum = 0.f;
-    for (int64_t first = 0; first < parts; first += 256) {
+    for (int64_t first = 0; first < parts; first += 4 * kLanes) {
         float2 v[4];
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            const int64_t p = first + 64 * k + lane;
+            const int64_t p = first + kLanes * k + lane;
             v[k] = p < parts ? s[p] : float2{-__builtin_inff(), 0.f};
         }
         float most = top;
@@ -329,15 +452,26 @@ __global__ __launch_bounds__(256) void join_loss(Tokens tokens, int64_t parts, i
         for (int k = 0; k < 4; k++) sum += v[k].y * expf(v[k].x - from);
         top = most;
     }
-    float all = top;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
-    const float from = all == -__builtin_inff() ? 0.f : all;
-    sum *= expf(top - from);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    const auto join = [&](int width) {
+        float all = top;
+        for (int d = width / 2; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+        const float from = all == -__builtin_inff() ? 0.f : all;
+        sum *= expf(top - from);
+        for (int d = width / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        top = all;
+    };
+    join(64);
+    if constexpr (WAVES > 1) {
+        __shared__ float2 waves[WAVES];
+        if ((lane & 63) == 0) waves[lane >> 6] = float2{top, sum};
+        __syncthreads();
+        const float2 v = waves[lane % WAVES];
+        top = v.x;
+        sum = v.y;
+        join(WAVES);
+    }
     if (lane != 0) return;
-    const float total = from + logf(sum);
+    const float total = (top == -__builtin_inff() ? 0.f : top) + logf(sum);
     lse[token] = total;
     loss[token] = tokens.target_of(row) < 0 ? __builtin_nanf("") : total - picked[row];
 }
@@ -607,6 +741,10 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
 // 300 x 2048 x 30000 with gradients 1450 and 1309, 2000 x 1500 x 5000 1133 and 1048, the loss of 509 x 768 x 30522 200 and 192.
 template <typename T, Layout LA, Layout LB>
 using Tiny = Tile<T, 64, 64, 4, 1, LA, LB>;
+// The tiny one with more of the weight on its way, for one row of tiles, whose blocks all run at a time, three on a compute unit.  Three
+// stages in LDS instead of two, us: 32 x 2048 x 50257 56 and 59 to 61, 64 x 2048 x 50257 56 and 59, 64 x 1024 x 50257 24.3 and 23.8.
+template <typename T, Layout LA, Layout LB>
+using Streamed = Tile<T, 64, 64, 4, 1, LA, LB, 3>;
 template <typename T, Layout LA, Layout LB>
 using Small = std::conditional_t<sizeof(T) == 2, Tile<T, 128, 128, 2, 2, LA, LB>, Tiny<T, LA, LB>>;
 template <typename T, Layout LA, Layout LB>
@@ -696,6 +834,21 @@ struct Calls {
             first, columns, l.parts, at<float2>(l.stats), at<float>(l.picked));
         launched();
     }
+    void loss_of_few() const
+    {
+        few_tiles<T><<<dim3(uint32_t((l.vocab + kFewColumns - 1) / kFewColumns)), 64 * kFewWaves, 0, stream>>>(
+            tokens(), static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.pitch, l.parts, at<float2>(l.stats),
+            at<float>(l.picked));
+        launched();
+    }
+    template <int WAVES>
+    void join(int side, float *loss, float *lse) const
+    {
+        constexpr int kPerBlock = join_tokens<WAVES>;
+        join_loss<WAVES><<<dim3(uint32_t((l.tokens + kPerBlock - 1) / kPerBlock)), 64 * WAVES * kPerBlock, 0, stream>>>(
+            tokens(), (l.vocab + side - 1) / side, l.parts, at<float2>(l.stats), at<float>(l.picked), loss, lse);
+        launched();
+    }
     bool direct() const { return l.tokens <= 64 && !l.padded; }
     Tokens tokens() const
     {
@@ -703,7 +856,14 @@ struct Calls {
     }
     hipError_t loss(float *loss, float *lse) const
     {
-        if (!direct()) list(nullptr, nullptr);
+        if (direct()) {
+            const bool few = l.tokens <= kFewTokens;
+            if (few) loss_of_few();
+            else loss_piece<Streamed<T, kSumContiguous, kSumStrips>>(0, l.vocab);
+            join<kJoinWaves>(few ? kFewColumns : 64, loss, lse);
+            return error;
+        }
+        list(nullptr, nullptr);
         // (a weight that needs no padding is walked in one launch)
         const int64_t piece = l.padded ? l.piece : l.vocab;
         const Size size = size_of<T>(l.tokens, piece);
@@ -713,10 +873,7 @@ struct Calls {
             else if (size == kSmall) loss_piece<Small<T, kSumContiguous, kSumStrips>>(first, columns);
             else loss_piece<Tiny<T, kSumContiguous, kSumStrips>>(first, columns);
         }
-        const int side = size == kLarge ? 256 : size == kSmall ? 128 : 64;
-        join_loss<<<dim3(uint32_t((l.tokens + 3) / 4)), 256, 0, stream>>>(tokens(), (l.vocab + side - 1) / side, l.parts, at<float2>(l.stats),
-                                                                      at<float>(l.picked), loss, lse);
-        launched();
+        join<1>(size == kLarge ? 256 : size == kSmall ? 128 : 64, loss, lse);
         return error;
     }
 

@@ -177,7 +177,7 @@ struct Side {
 //   m = 16 i + lane % 16 (+ the wave's first row), n = 16 j + 4 (lane / 16) + e (+ the wave's first column):
 // four neighbouring columns of a row (the side of the columns is the instruction's first operand).  With kSumStrips columns
 // n = 16 (lane / 16) + 4 j + e: sixteen neighbouring ones, which an epilogue of 16-bit elements stores 16 bytes at a time.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, Layout LA, Layout LB>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, Layout LA, Layout LB, int STAGES = 2>
 struct Tile {
     using T = T_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
@@ -188,7 +188,7 @@ struct Tile {
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     static_assert(LB != kSumStrips || TN == 4, "strips are as wide as a wave's columns");
     static constexpr int kStage = A::kBytes + B::kBytes;
-    static constexpr int kLds = 2 * kStage;
+    static constexpr int kLds = STAGES * kStage;
 
     f32x4 acc[TM][TN];
     int wave, lane, wm, wn;
@@ -226,7 +226,17 @@ struct Tile {
     }
     static constexpr int kReads = TM * A::kReadsPerFragment + TN * B::kReadsPerFragment;
 
-    // One step: the products of the stage at `now`, whose first half is in f0 already.  LOAD: the step after the next one follows and
+    // Waits for the oldest stage that is on its way (MORE: others are, and may stay so) and for LDS reads.
+    template <bool MORE>
+    static __device__ __forceinline__ void wait()
+    {
+        constexpr int kLater = MORE ? (STAGES - 2) * (A::kLoads + B::kLoads) : 0;
+        static_assert(kLater < 16, "a count of four bits");
+        __builtin_amdgcn_s_waitcnt(0x0070 | kLater);
+    }
+    static __device__ __forceinline__ uint32_t next(uint32_t now) { return STAGES == 2 ? kStage - now : now == (STAGES - 1) * kStage ? 0 : now + kStage; }
+
+    // One step: the products of the stage at `now`, whose first half is in f0 already.  LOAD: the step STAGES steps on exists and
     // is loaded into the same place; NEXT: another step follows, its first half is fetched into f0.
     template <bool LOAD, bool NEXT>
     __device__ __forceinline__ void step(A &a, B &b, Frags &f0, Frags &f1, const unsigned char *lds, uint32_t at, uint32_t now)
@@ -238,23 +248,22 @@ struct Tile {
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (NEXT) {
             // the next stage is here, and everybody is done reading this one
-            wait_loads_and_reads();
+            wait<LOAD>();
             barrier();
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (LOAD) {
                 a.load(at + now, wave);
                 b.load(at + now + A::kBytes, wave);
             }
-            fetch(f0, lds + (kStage - now), 0);
+            fetch(f0, lds + next(now), 0);
         }
         multiply(f1);
         interleave<NEXT ? kReads : 0, LOAD ? A::kLoads + B::kLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
     }
-    static __device__ __forceinline__ void wait_loads_and_reads() { __builtin_amdgcn_s_waitcnt(0x0070); }
 
     // steps: of kDepth each; the last one has `last` elements of the summed axis (kRowContiguous sides).
-    // Two stages in LDS: the loads that fill one are issued half a step after its last read, a whole step before they are waited for.
+    // Stages in LDS: the loads that fill one are issued half a step after its last read, STAGES - 1 steps before they are waited for.
     __device__ __forceinline__ void run(A &a, B &b, int steps, int last, unsigned char *lds)
     {
         const int tid = int(threadIdx.x);
@@ -275,32 +284,38 @@ struct Tile {
         };
         const uint32_t at = lds_address(lds);
         uint32_t now = 0;
-        if (steps == 1) shorten();
-        a.load(at, wave);
-        b.load(at + A::kBytes, wave);
-        wait_loads_and_reads();
+        const auto first = [&](int s) {
+            if (s >= steps) return;
+            if (s == steps - 1) shorten();
+            a.load(at + s * kStage, wave);
+            b.load(at + s * kStage + A::kBytes, wave);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; s++) first(s);
+        if (steps >= STAGES - 1) wait<true>();
+        else wait<false>();
         barrier();
-        if (steps > 1) {
-            if (steps == 2) shorten();
-            a.load(at + kStage, wave);
-            b.load(at + kStage + A::kBytes, wave);
-        }
+        first(STAGES - 1);
         Frags f0, f1;
         fetch(f0, lds, 0);
         int s = 0;
-        for (; s + 3 < steps; s++) {
+        for (; s + STAGES + 1 < steps; s++) {
             step<true, true>(a, b, f0, f1, lds, at, now);
-            now = kStage - now;
+            now = next(now);
         }
-        if (s + 2 < steps) {
+        if (s + STAGES < steps) {
             shorten();
             step<true, true>(a, b, f0, f1, lds, at, now);
-            now = kStage - now;
+            now = next(now);
             s++;
         }
-        if (s + 1 < steps) {
-            step<false, true>(a, b, f0, f1, lds, at, now);
-            now = kStage - now;
+#pragma unroll
+        for (int k = 1; k < STAGES; k++) {
+            if (s + 1 < steps) {
+                step<false, true>(a, b, f0, f1, lds, at, now);
+                now = next(now);
+                s++;
+            }
         }
         step<false, false>(a, b, f0, f1, lds, at, now);
     }

@@ -294,3 +294,38 @@ def test_a_means_factor_is_not_rounded_in_every_target(torch, tokens, dtype):
     for name, want in (("dhidden", torch.mm(d, w) / tokens), ("dweight", torch.mm(d.t().contiguous(), x) / tokens)):
         off, rounded = (float((t.double() - want).norm() / want.norm()) for t in (got[name], want.to(hidden.dtype)))
         assert off <= rounded + 2.0 / vocab + 0.05 * ROUNDOFF[dtype], (name, off, rounded)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [64, 128, 192, 320, 1088])
+@pytest.mark.parametrize("tokens", [1, 15, 16, 17, 33, 64])
+def test_few_tokens_at_the_ends_of_tiles_and_quarters(torch, tokens, width, dtype):
+    # widths of 1 to 17 units of 128 bytes (2 to 34 for f32): quarters that are empty, odd, uneven
+    for vocab in (1, 31, 33, 64, 1003):
+        hidden, weight, targets = inputs(torch, tokens, width, vocab, dtype, seed=tokens + width + vocab)
+        targets[tokens // 2] = -100 if tokens > 1 else targets[0]
+        check(torch, hidden, weight, targets)
+
+
+@pytest.mark.parametrize("tokens", [2, 20])
+def test_few_tokens_over_more_parts_than_one_pass_joins(torch, tokens):
+    # 16 waves of a token's block take 4096 parts at a time: 131072 columns in blocks of 32, 262144 in tiles of 64
+    hidden, weight, targets = inputs(torch, tokens, 64, 300007, "bf16", seed=3)
+    targets[0], targets[1] = 300006, 262144
+    check(torch, hidden, weight, targets)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [7, 40])
+def test_a_tokens_nan_and_infinity_stay_its_own(torch, tokens, dtype):
+    hidden, weight, targets = inputs(torch, tokens, 256, 500, dtype, seed=tokens)
+    targets[2] = -100
+    clean = call(torch, hidden, weight, targets)
+    bad = hidden.clone()
+    bad[2, 5] = math.nan                                 # of a token that does not count
+    bad[4, 200] = math.nan
+    bad[5, 0] = math.inf
+    got = call(torch, bad, weight, targets)
+    assert torch.isnan(got["loss"][4]) and torch.isnan(got["loss"][5])
+    keep = [k for k in range(tokens) if k not in (4, 5)]
+    assert torch.equal(got["loss"][keep], clean["loss"][keep]) and torch.equal(got["lse"][keep], clean["lse"][keep])
