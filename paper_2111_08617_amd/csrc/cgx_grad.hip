@@ -130,6 +130,7 @@ __device__ __forceinline__ double block_sum(double v, double *waves)
 
 // A block's share of the squares: items block, block + grid, ... of the launch.  Squares of binary32 values are exact in binary64,
 // so nothing overflows and only the additions round; no atomics, so a norm is the same bits every time.
+// 2.2 GB of bfloat16: 330 us (6.7 TB/s); 102 MB of binary32 17 us (6 TB/s); some tens of small tensors 3.5 us.
 template <bool STREAM>
 __global__ __launch_bounds__(kBlock) void norm_items(Group group, double *partial, int32_t add)
 {
@@ -187,7 +188,9 @@ __device__ __forceinline__ void scale_item(const void *src, int64_t from, void *
     if (at < n) q[at] = Result(float(p[at]) * factor);
 }
 
-// x * factor, in place (OUT < 0: each tensor in its own type) or into the fused buffer.
+// x * factor, in place (OUT < 0: each tensor in its own type) or into the fused buffer.  factor = min(1, max_norm / norm) in binary32;
+// the product is rounded once, to the result's type.  2.2 GB of bfloat16 into 4.4 GB of binary32: 1128 us (5.8 TB/s; a copy of 4 GB
+// by the library 4.75); 102 MB of binary32, which the norm has left in the memory-side cache, 31 us (6.5 TB/s).
 template <int OUT, bool STREAM>
 __global__ __launch_bounds__(kBlock) void clip_items(Group group, const float *norm, float max_norm, void *out)
 {
