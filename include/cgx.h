@@ -420,7 +420,7 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
  *   workspace device, 16-byte aligned, at least the bytes cgx_head_workspace reports (CGX_ERR_SIZE
  *             otherwise); contents unspecified before and after.  Calls that share one must not overlap.
  * Outputs overlap no input.  tokens may be 0 (dweight is then zero); 1 <= width <= 2^17, 1 <= vocab < 2^31,
- * tokens < 2^24, and tokens * vocab as well as tokens * width about 2^36 at most (CGX_ERR_SIZE).
+ * tokens < 2^24, and tokens, rounded up to a multiple of 256, times vocab or times width below 2^36 (CGX_ERR_SIZE).
  */
 int cgx_head_workspace(int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt,
                        int32_t grad /* 0: for cgx_head_loss; else for both calls */, size_t *bytes);

@@ -11,7 +11,8 @@ namespace cgx {
 constexpr int kHeadRows = 256;                       // token rows and columns of a piece come in multiples of it (the largest tile)
 constexpr int kHeadBlocks = 256;                     // compute units: a sum is split into parts where its tiles are fewer
 constexpr size_t kHeadHeaderBytes = 256;
-constexpr int kFewTokens = 16;                       // up to this many, the loss has a kernel of its own, a block of it for
+constexpr int kDirectTokens = 64;                    // up to this many tokens the loss can take as they come
+constexpr int kFewTokens = 16;                       // a block of its kernel for few tokens takes this many, and
 constexpr int kFewColumns = 32;                      // this many columns of the vocabulary
 
 inline size_t head_element(int dt) { return dt == CGX_F32 ? 4 : 2; }

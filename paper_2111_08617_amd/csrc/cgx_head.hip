@@ -71,37 +71,24 @@ struct Padding {
 template <typename T>
 __device__ __forceinline__ void copy_row(const T *src, int64_t width, T *dst, int64_t pitch, int thread, int threads)
 {
-    constexpr int kPer = 16 / int(sizeof(T));
-    typedef uint32_t Vec __attribute__((ext_vector_type(4)));
-    // (eight loads on their way at a time)
-    constexpr int kAhead = 8;
-    if (!src || width % kPer == 0) {
-        for (int64_t from = int64_t(thread) * kPer; from < pitch; from += int64_t(threads) * kPer * kAhead) {
-            Vec v[kAhead];
+    constexpr int kPer = 16 / int(sizeof(T)), kAhead = 8;       // (eight loads on their way at a time)
+    typedef T Vec __attribute__((ext_vector_type(kPer)));
+    typedef Vec Anywhere __attribute__((aligned(sizeof(T))));
+    for (int64_t from = int64_t(thread) * kPer; from < pitch; from += int64_t(threads) * kPer * kAhead) {
+        Vec v[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; i++) {
-                const int64_t k = from + int64_t(i) * threads * kPer;
-                v[i] = src && k < width ? *reinterpret_cast<const Vec *>(src + k) : Vec{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; i++) {
-                const int64_t k = from + int64_t(i) * threads * kPer;
-                if (k < pitch) *reinterpret_cast<Vec *>(dst + k) = v[i];
-            }
+        for (int i = 0; i < kAhead; i++) {
+            const int64_t k = from + int64_t(i) * threads * kPer;
+            v[i] = Vec(T(0.f));
+            if (!src || k >= width) continue;
+            if (k + kPer <= width) v[i] = *reinterpret_cast<const Anywhere *>(src + k);
+            else
+                for (int e = 0; e < kPer; e++) v[i][e] = k + e < width ? src[k + e] : T(0.f);
         }
-    } else {
-        for (int64_t from = thread; from < pitch; from += int64_t(threads) * kAhead) {
-            T v[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; i++) {
-                const int64_t k = from + int64_t(i) * threads;
-                v[i] = k < width ? src[k] : T(0.f);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; i++) {
-                const int64_t k = from + int64_t(i) * threads;
-                if (k < pitch) dst[k] = v[i];
-            }
+        for (int i = 0; i < kAhead; i++) {
+            const int64_t k = from + int64_t(i) * threads * kPer;
+            if (k < pitch) *reinterpret_cast<Vec *>(dst + k) = v[i];
         }
     }
 }
@@ -331,7 +318,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
     }
 }
 
-// The same for up to 16 tokens, where reading W is all that takes time: a block per kFewColumns rows of W, whose four waves each sum a
+// The same for few tokens, where reading W is all that takes time: a block per 16 tokens and kFewColumns rows of W, whose four waves each sum a
 // quarter of the width.  W goes from memory to the registers of the one wave that uses it, a unit of 128 bytes per row ahead of the products,
 // so there are no barriers on the way and every wave has its own loads in flight; tokens are read from the caches, at half of W's bytes.
 // Calls with it and with tiny tiles, us: 1 x 2048 x 50257 bfloat16 (206 MB) 44 and 56, 1 x 4096 x 50257 82 and 96, 16 x 2048 x 50257 48 and 60,
@@ -341,34 +328,36 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
 constexpr int kFewWaves = 4;
 template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, const T *__restrict__ hidden, const T *__restrict__ weight,
-                                                               int64_t pitch, int64_t parts, float2 *__restrict__ stats,
+                                                               int64_t width, uint32_t groups, int64_t parts, float2 *__restrict__ stats,
                                                                float *__restrict__ picked)
 {
     using E = Element<T>;
     using Frag = typename E::Frag;
+    typedef Frag Anywhere __attribute__((aligned(sizeof(T))));         // (rows start at any element)
     constexpr int TN = kFewColumns / 16, kUnit = kStepBytes / int(sizeof(T)), kPitch = kFewColumns + 4;
     __shared__ __align__(16) float part[kFewWaves][16][kPitch];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
-    const int64_t n0 = int64_t(blockIdx.x) * kFewColumns;
-    const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens);
+    const uint32_t block = blockIdx.x / groups;
+    const int64_t n0 = int64_t(block) * kFewColumns, m0 = int64_t(blockIdx.x % groups) * kFewTokens;
+    const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens - m0);
     // (rows past the last one are read from it, and not used)
     uint32_t of_column[TN];
-    const uint32_t of_token = uint32_t(r < count ? r : count - 1) * uint32_t(pitch * sizeof(T)) + g * 16;
+    const uint32_t of_token = uint32_t(r < count ? r : count - 1) * uint32_t(width * sizeof(T)) + g * 16;
 #pragma unroll
-    for (int j = 0; j < TN; j++) of_column[j] = uint32_t(16 * j + r < columns ? 16 * j + r : columns - 1) * uint32_t(pitch * sizeof(T)) + g * 16;
+    for (int j = 0; j < TN; j++) of_column[j] = uint32_t(16 * j + r < columns ? 16 * j + r : columns - 1) * uint32_t(width * sizeof(T)) + g * 16;
     struct Unit {
         Frag a[2], b[2][TN];
     };
-    const int units = int(pitch / kUnit), from = units * wave / kFewWaves, to = units * (wave + 1) / kFewWaves;
-    const unsigned char *w = reinterpret_cast<const unsigned char *>(weight + n0 * pitch), *x = reinterpret_cast<const unsigned char *>(hidden);
+    const int units = int(width / kUnit), from = units * wave / kFewWaves, to = units * (wave + 1) / kFewWaves;
+    const unsigned char *w = reinterpret_cast<const unsigned char *>(weight + n0 * width), *x = reinterpret_cast<const unsigned char *>(hidden + m0 * width);
     const auto load = [&](Unit &u, int at) {
 #pragma unroll
         for (int half = 0; half < 2; half++)
 #pragma unroll
-            for (int j = 0; j < TN; j++) u.b[half][j] = *reinterpret_cast<const Frag *>(w + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_column[j]);
+            for (int j = 0; j < TN; j++) u.b[half][j] = *reinterpret_cast<const Anywhere *>(w + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_column[j]);
 #pragma unroll
         for (int half = 0; half < 2; half++)
-            u.a[half] = *reinterpret_cast<const Frag *>(x + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_token);
+            u.a[half] = *reinterpret_cast<const Anywhere *>(x + int64_t(at) * kStepBytes + half * (kStepBytes / 2) + of_token);
     };
     f32x4 acc[TN];
 #pragma unroll
@@ -397,20 +386,39 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
         multiply(u0);
         if (at + 1 < to) multiply(u1);
     }
+    const int rest = int(width % kUnit);
+    if (rest && wave == kFewWaves - 1) {                 // the width's last, partial unit
+        Unit u;
+        const auto load_rest = [&](const unsigned char *p, int half) {
+            Frag v;
+#pragma unroll
+            for (int e = 0; e < 16 / int(sizeof(T)); e++)
+                v[e] = half * (kUnit / 2) + g * (16 / int(sizeof(T))) + e < rest ? reinterpret_cast<const T *>(p)[e] : T(0.f);
+            return v;
+        };
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            const int64_t at = int64_t(units) * kStepBytes + half * (kStepBytes / 2);
+#pragma unroll
+            for (int j = 0; j < TN; j++) u.b[half][j] = load_rest(w + at + of_column[j], half);
+            u.a[half] = load_rest(x + at + of_token, half);
+        }
+        multiply(u);
+    }
 #pragma unroll
     for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(&part[wave][r][16 * j + 4 * g]) = acc[j];
     __syncthreads();
     // a token's columns: kLanes neighbouring lanes, kEach columns a lane
     constexpr int kEach = 16 * kFewColumns / (64 * kFewWaves), kLanes = kFewColumns / kEach;
     const int m = tid / kLanes, first = tid % kLanes * kEach;
-    const int32_t target = m < count ? tokens.target_of(m) : -1;
+    const int32_t target = m < count ? tokens.target_of(m0 + m) : -1;
     float z[kEach], top = -__builtin_inff();
 #pragma unroll
     for (int e = 0; e < kEach; e++) {
         z[e] = 0.f;
 #pragma unroll
         for (int k = 0; k < kFewWaves; k++) z[e] += part[k][m][first + e];
-        if (m < count && target == n0 + first + e) picked[m] = z[e];
+        if (m < count && target == n0 + first + e) picked[m0 + m] = z[e];
         if (first + e >= columns) z[e] = -__builtin_inff();
         top = fmaxf(top, z[e]);
     }
@@ -422,7 +430,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
     for (int e = 0; e < kEach; e++) sum += exp_from<T>(z[e], base);
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-    if (m < count && first == 0) stats[m * parts + blockIdx.x] = float2{top, sum};
+    if (m < count && first == 0) stats[(m0 + m) * parts + block] = float2{top, sum};
 }
 
 // Joins the parts of every token's softmax: a wave per token, four of them in a block, or (few tokens) a block of many waves per token.
@@ -635,9 +643,10 @@ __device__ __forceinline__ void store_weights(T *dweight, int64_t row, int64_t c
     Four out;
 #pragma unroll
     for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
+    typedef Four Anywhere __attribute__((aligned(sizeof(T))));          // (rows start at any element)
     T *p = dweight + row * width + column;
-    if (width % 4 == 0) {
-        *reinterpret_cast<Four *>(p) = out;
+    if (column + 4 <= width) {
+        *reinterpret_cast<Anywhere *>(p) = out;
     } else {
 #pragma unroll
         for (int e = 0; e < 4; e++)
@@ -727,6 +736,7 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
                                                     T *__restrict__ dhidden)
 {
     typedef T Four __attribute__((ext_vector_type(4)));
+    typedef Four Anywhere __attribute__((aligned(sizeof(T))));          // (rows start at any element)
     const int64_t token = blockIdx.x, count = header->count;
     const int32_t row = place[token];
     const float unscale = header->unscale;
@@ -738,8 +748,8 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
         Four out;
 #pragma unroll
         for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
-        if (width % 4 == 0) {
-            *reinterpret_cast<Four *>(d + k) = out;
+        if (k + 4 <= width) {
+            *reinterpret_cast<Anywhere *>(d + k) = out;
         } else {
 #pragma unroll
             for (int e = 0; e < 4; e++)
@@ -851,8 +861,9 @@ struct Calls {
     }
     void loss_of_few() const
     {
-        few_tiles<T><<<dim3(uint32_t((l.vocab + kFewColumns - 1) / kFewColumns)), 64 * kFewWaves, 0, stream>>>(
-            tokens(), static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.pitch, l.parts, at<float2>(l.stats),
+        const uint32_t groups = uint32_t((l.tokens + kFewTokens - 1) / kFewTokens);
+        few_tiles<T><<<dim3(uint32_t((l.vocab + kFewColumns - 1) / kFewColumns) * groups), 64 * kFewWaves, 0, stream>>>(
+            tokens(), static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.width, groups, l.parts, at<float2>(l.stats),
             at<float>(l.picked));
         launched();
     }
@@ -864,7 +875,12 @@ struct Calls {
             tokens(), (l.vocab + side - 1) / side, l.parts, at<float2>(l.stats), at<float>(l.picked), loss, lse);
         launched();
     }
-    bool direct() const { return l.tokens <= 64 && !l.padded; }
+    // Tokens of few_tiles: it reads rows that start anywhere, which the tiles need padded, at three times the weight's traffic; a second group of
+    // 16 tokens takes the weight again.  us with it and with padding: 16 x 1198 x 50257 bfloat16 31 and 84, 32 x 1198 x 50257 52 and 79, 64 x
+    // 1198 x 50257 94 and 83; rows of an odd number of 16-bit elements, whose loads cost more, 1 x 1537 x 50257 75 and 96, 16 x 1537 x 50257
+    // 105 and 96, 16 x 1537 x 5000 22 and 27, 48 x 1537 x 5000 36 and 27.
+    bool few() const { return l.tokens <= (l.padded && l.width * sizeof(T) % 4 == 0 ? 2 * kFewTokens : kFewTokens); }
+    bool direct() const { return few() || (l.tokens <= kDirectTokens && !l.padded); }
     Tokens tokens() const
     {
         return Tokens{direct() ? nullptr : header(), at<int32_t>(l.place), at<int32_t>(l.target), b.targets, l.tokens, b.ignore, l.vocab};
@@ -872,10 +888,9 @@ struct Calls {
     hipError_t loss(float *loss, float *lse) const
     {
         if (direct()) {
-            const bool few = l.tokens <= kFewTokens;
-            if (few) loss_of_few();
+            if (few()) loss_of_few();
             else loss_piece<Streamed<T, kSumContiguous, kSumStrips>>(0, l.vocab);
-            join<kJoinWaves>(few ? kFewColumns : 64, loss, lse);
+            join<kJoinWaves>(few() ? kFewColumns : 64, loss, lse);
             return error;
         }
         list(nullptr, nullptr);

@@ -329,3 +329,12 @@ def test_a_tokens_nan_and_infinity_stay_its_own(torch, tokens, dtype):
     assert torch.isnan(got["loss"][4]) and torch.isnan(got["loss"][5])
     keep = [k for k in range(tokens) if k not in (4, 5)]
     assert torch.equal(got["loss"][keep], clean["loss"][keep]) and torch.equal(got["lse"][keep], clean["lse"][keep])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [1, 7, 31, 33, 63, 65, 72, 127, 129, 321, 1766])
+def test_few_tokens_of_any_width(torch, width, dtype):
+    # rows that start at any element, with a last unit of every kind; nothing past the weight's end is read (its last row ends an allocation's use)
+    for tokens, vocab in ((1, 1), (3, 65), (16, 130), (17, 33), (50, 97), (64, 31)):
+        hidden, weight, targets = inputs(torch, tokens, width, vocab, dtype, seed=tokens + width)
+        check(torch, hidden, weight, targets)
