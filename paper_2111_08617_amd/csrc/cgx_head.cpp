@@ -35,7 +35,7 @@ int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad,
     l.piece = up((vocab + l.pieces - 1) / l.pieces, kHeadRows);
     l.pieces = (vocab + l.piece - 1) / l.piece;
     // columns of the narrowest tile, or of a block of the kernel for few tokens
-    const int64_t narrowest = tokens <= kDirectTokens ? kFewColumns : 64;
+    const int64_t narrowest = tokens <= kDirectTokens || ((tokens + 63) / 64) * ((vocab + 63) / 64) <= kFewTiles ? kFewColumns : 64;
     l.parts = (vocab + narrowest - 1) / narrowest;
     size_t at = kHeadHeaderBytes;
     const auto take = [&at](int64_t bytes) {

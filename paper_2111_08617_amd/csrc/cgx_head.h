@@ -14,6 +14,7 @@ constexpr size_t kHeadHeaderBytes = 256;
 constexpr int kDirectTokens = 64;                    // up to this many tokens the loss can take as they come
 constexpr int kFewTokens = 16;                       // a block of its kernel for few tokens takes this many, and
 constexpr int kFewColumns = 32;                      // this many columns of the vocabulary
+constexpr int kFewTiles = 64;                        // it also takes calls of up to this many tiles of 64 x 64 logits
 
 inline size_t head_element(int dt) { return dt == CGX_F32 ? 4 : 2; }
 // Elements of the summed axis per step of the products: rows are padded to a multiple of it.

@@ -53,7 +53,7 @@ __device__ __forceinline__ float lifted(float z, float from)
 // number of tokens that count, of those ahead of its own, and the largest factor; then it lists and copies its own.  Blocks past the
 // first list_blocks pad rows of the weight meanwhile, where these have to be (see HeadLayout::padded).
 // 4096 tokens of 768 bfloat16 elements, 15 % of which count: 7.5 us; 8192 that all count, and are not copied: 9.2 us; 125 of 519 binary32
-// elements and a weight of 1003 rows to pad: 8 us.  All of it is latency: a launch, two dependent loads, two barriers.
+// elements and a weight of 1003 rows to pad: 7.5 us.  All of it is latency: a launch, two dependent loads, two barriers.
 constexpr int kListThreads = 1024, kListWaves = kListThreads / 64, kListEach = 8;
 
 struct Lists {
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
     }
 }
 
-// The same for few tokens, where reading W is all that takes time: a block per 16 tokens and kFewColumns rows of W, whose four waves each sum a
+// The same for few tokens, where reading W is all that takes time, and for few logits: a block per 16 tokens and kFewColumns rows of W, whose four waves each sum a
 // quarter of the width.  W goes from memory to the registers of the one wave that uses it, a unit of 128 bytes per row ahead of the products,
 // so there are no barriers on the way and every wave has its own loads in flight; tokens are read from the caches, at half of W's bytes.
 // Calls with it and with tiny tiles, us: 1 x 2048 x 50257 bfloat16 (206 MB) 44 and 56, 1 x 4096 x 50257 82 and 96, 16 x 2048 x 50257 48 and 60,
@@ -879,7 +879,15 @@ struct Calls {
     // 16 tokens takes the weight again.  us with it and with padding: 16 x 1198 x 50257 bfloat16 31 and 84, 32 x 1198 x 50257 52 and 79, 64 x
     // 1198 x 50257 94 and 83; rows of an odd number of 16-bit elements, whose loads cost more, 1 x 1537 x 50257 75 and 96, 16 x 1537 x 50257
     // 105 and 96, 16 x 1537 x 5000 22 and 27, 48 x 1537 x 5000 36 and 27.
-    bool few() const { return l.tokens <= (l.padded && l.width * sizeof(T) % 4 == 0 ? 2 * kFewTokens : kFewTokens); }
+    // Where tiles would leave most of the chip idle it has eight times as many blocks, a quarter of the sums each, and needs no list.  us with it
+    // and with tiles: 125 x 519 x 1003 binary32 (32 tiles) 12.7 and 24.5, 256 x 1024 x 1000 bfloat16 (64) 13 and 17, binary32 19 and 30; 256 x
+    // 1024 x 2000 bfloat16 (128) 18 and 17, 256 x 1024 x 4000 (252) 28.7 and 18; rows of an odd number of 16-bit elements, 100 x 1537 x 2000 (64),
+    // 35 and 27.
+    bool few() const
+    {
+        const bool words = l.width * sizeof(T) % 4 == 0;
+        return l.tokens <= (l.padded && words ? 2 * kFewTokens : kFewTokens) || (words && tiles(l.tokens, l.vocab, 64) <= kFewTiles);
+    }
     bool direct() const { return few() || (l.tokens <= kDirectTokens && !l.padded); }
     Tokens tokens() const
     {

@@ -338,3 +338,13 @@ def test_few_tokens_of_any_width(torch, width, dtype):
     for tokens, vocab in ((1, 1), (3, 65), (16, 130), (17, 33), (50, 97), (64, 31)):
         hidden, weight, targets = inputs(torch, tokens, width, vocab, dtype, seed=tokens + width)
         check(torch, hidden, weight, targets)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(65, 96, 1), (256, 1024, 1000), (257, 130, 769), (1000, 66, 255), (4096, 64, 64), (4097, 64, 64), (100, 519, 2000)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_few_logits_of_many_tokens(torch, shape, dtype):
+    hidden, weight, targets = inputs(torch, *shape, dtype, seed=sum(shape))
+    targets[1::3] = -100
+    hidden[4] = math.nan                                 # (4 = 1 + 3: does not count)
+    check(torch, hidden, weight, targets)
