@@ -217,8 +217,8 @@ struct Hidden {
     __device__ __forceinline__ const T *of(int64_t count) const { return own && count == tokens ? own : listed; }
 };
 
-// The tokens of a loss call: listed, or as they come.  Few tokens are one row of tiles whether all of them count or not, and need no list
-// (a launch of 6 us beside 18 us for one token's logits); those that do not count get a loss of 0 in the end.
+// The tokens of a loss call: listed, or as they come.  Few tokens or few logits take the same time whether all of them count or not, and
+// need no list (a launch of 6 us beside 18 us for one token's logits); tokens that do not count get a loss of 0 in the end.
 struct Tokens {
     const Header *header;    // null: as they come
     const int32_t *place, *target;
@@ -886,7 +886,8 @@ struct Calls {
     bool few() const
     {
         const bool words = l.width * sizeof(T) % 4 == 0;
-        return l.tokens <= (l.padded && words ? 2 * kFewTokens : kFewTokens) || (words && tiles(l.tokens, l.vocab, 64) <= kFewTiles);
+        const bool twice = l.padded && words && l.vocab < int64_t(1) << 27;      // (two groups' grid stays under 2^32 threads)
+        return l.tokens <= (twice ? 2 * kFewTokens : kFewTokens) || (words && tiles(l.tokens, l.vocab, 64) <= kFewTiles);
     }
     bool direct() const { return few() || (l.tokens <= kDirectTokens && !l.padded); }
     Tokens tokens() const
