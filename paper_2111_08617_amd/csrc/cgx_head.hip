@@ -50,7 +50,7 @@ __device__ __forceinline__ float lifted(float z, float from)
 // A token takes part if its target is not `ignore` and (gradient) its factor is not 0; the products then run over that list alone.
 //
 // One launch does both: every block looks at all targets (a few loads per thread for some thousand tokens, against a launch's 3 us) for the
-// number of tokens that count, of those ahead of its own, and the largest factor; then it lists and copies its own.  Blocks past the
+// number of tokens that count, of those ahead of its own, and the largest finite factor; then it lists and copies its own.  Blocks past the
 // first list_blocks pad rows of the weight meanwhile, where these have to be (see HeadLayout::padded).
 // 4096 tokens of 768 bfloat16 elements, 15 % of which count: 7.5 us; 8192 that all count, and are not copied: 9.2 us; 125 of 519 binary32
 // elements and a weight of 1003 rows to pad: 7.5 us.  All of it is latency: a launch, two dependent loads, two barriers.
@@ -153,7 +153,8 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
             if (v[k] == ignore || g[k] == 0.f) continue;
             mine.all++;
             mine.before += from + k * kListThreads + tid < first;
-            mine.top = fmaxf(mine.top, fabsf(g[k]));
+            const float size = fabsf(g[k]);
+            if (size < __builtin_inff()) mine.top = fmaxf(mine.top, size);       // (neither infinities nor NaN)
         }
     }
     const Totals t = block_totals(mine, totals);
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
     // no probability yet then is exactly -2^top_bits, and near 1 the rounding is at its finest: in units of 1 all targets of a call
     // would be off by the same rounding of the factor, and with them the whole gradient, by up to 2^-8.  In binary16, with 14, probabilities down to
     // 1e-9 stay normal numbers and nothing overflows, whatever the loss scale.
-    const float unit = !top_bits || !(t.top < __builtin_inff()) || t.top == 0.f ? 1.f : fmaxf(t.top, 0x1p-100f);
+    // A factor that is not finite makes its own token's d so; the unit comes from the others, whose dhidden is none the worse for it.
+    const float unit = !top_bits || t.top == 0.f ? 1.f : fmaxf(t.top, 0x1p-100f);
     if (blockIdx.x == 0 && tid == 0) *header = Header{t.all, ldexpf(unit, -top_bits)};
     const bool copies = !(in_place && t.all == tokens);
     int32_t done = t.before;

@@ -348,3 +348,21 @@ def test_few_logits_of_many_tokens(torch, shape, dtype):
     targets[1::3] = -100
     hidden[4] = math.nan                                 # (4 = 1 + 3: does not count)
     check(torch, hidden, weight, targets)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("size", [1.0, 100.0, 1e-30])
+def test_a_factor_that_is_not_finite_stays_its_tokens(torch, size, bad, dtype):
+    """dhidden of a token depends on its own factor: those of the others are the same as where the token takes no part, in every bit,
+    as the units of d come from the finite factors either way.  (dweight is a sum over all tokens and is not finite by the formula.)"""
+    tokens, at = 90, 41
+    hidden, weight, targets = inputs(torch, tokens, 64, 333, dtype, seed=21)
+    dloss = torch.linspace(-size, size, tokens, device="cuda")
+    others = torch.arange(tokens, device="cuda") != at
+    dloss[at] = 0.0
+    want = check(torch, hidden, weight, targets, dloss)
+    dloss[at] = bad
+    got = call(torch, hidden, weight, targets, dloss)
+    assert torch.equal(got["dhidden"][others], want["dhidden"][others])
+    assert not got["dhidden"][at].isfinite().any()
