@@ -419,8 +419,9 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
  *   dhidden, dweight   device, tokens x width and vocab x width elements of dt; every element is written
  *   workspace device, 16-byte aligned, at least the bytes cgx_head_workspace reports (CGX_ERR_SIZE
  *             otherwise); contents unspecified before and after.  Calls that share one must not overlap.
- * Outputs overlap no input.  tokens may be 0 (dweight is then zero); 1 <= width <= 2^17, 1 <= vocab < 2^31,
- * tokens < 2^24, and tokens, rounded up to a multiple of 256, times vocab or times width below 2^36 (CGX_ERR_SIZE).
+ * Outputs overlap no input.  tokens may be 0 (dweight is then zero); 0 <= tokens < 2^24, 1 <= width <= 2^17, 1 <= vocab,
+ * and the tokens, rounded up to a multiple of 256 (one at least), times vocab or times width, both rounded up to a multiple
+ * of 64, below 2^36, so that a launch can hold them: vocab <= 2^28 - 64 for up to 256 tokens (CGX_ERR_SIZE otherwise).
  */
 int cgx_head_workspace(int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt,
                        int32_t grad /* 0: for cgx_head_loss; else for both calls */, size_t *bytes);

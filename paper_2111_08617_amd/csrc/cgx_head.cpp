@@ -15,7 +15,7 @@ constexpr int64_t kDeltaBytes = int64_t(512) << 20;
 int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad, HeadLayout *out)
 {
     if (dt != CGX_F32 && dt != CGX_F16 && dt != CGX_BF16) return CGX_ERR_DTYPE;
-    if (tokens < 0 || tokens >= (int64_t(1) << 24) || width < 1 || width > (1 << 17) || vocab < 1 || vocab >= (int64_t(1) << 31) - kHeadRows)
+    if (tokens < 0 || tokens >= (int64_t(1) << 24) || width < 1 || width > (1 << 17) || vocab < 1 || vocab >= int64_t(1) << 28)
         return CGX_ERR_SIZE;
     const int64_t size = int64_t(head_element(dt));
     HeadLayout l;
@@ -26,8 +26,8 @@ int head_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, bool grad,
     l.rows = up(tokens > 0 ? tokens : 1, kHeadRows);
     l.pitch = up(width, head_depth(dt));
     l.padded = l.pitch != width;
-    // a launch has a block of 256 threads per 64 x 64 results at most, and fewer than 2^32 threads
-    if (l.rows * vocab >= int64_t(1) << 36 || l.rows * l.pitch >= int64_t(1) << 36) return CGX_ERR_SIZE;
+    // a launch has a block of 256 threads per 64 x 64 results, begun ones among them, at most, and fewer than 2^32 threads
+    if (l.rows * up(vocab, 64) >= int64_t(1) << 36 || l.rows * up(width, 64) >= int64_t(1) << 36) return CGX_ERR_SIZE;
     // pieces of about the same length; at most 2^18 columns, so that byte offsets within a tile's rows fit 32 bits
     int64_t most = kDeltaBytes / (l.rows * size) / kHeadRows * kHeadRows;
     most = most < kHeadRows ? kHeadRows : most > (1 << 18) ? (1 << 18) : most;

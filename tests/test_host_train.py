@@ -192,3 +192,32 @@ def test_workspace_layout_is_clean_under_asan_and_ubsan(tmp_path):
                     os.path.join(os.path.dirname(here), "paper_2111_08617_amd", "csrc", "cgx_head.cpp"), "-o", exe], check=True)
     run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert run.returncode == 0 and "all checks passed" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
+
+
+def test_head_sizes_whose_last_tiles_make_the_launch_too_large(lib):
+    """A grid has tiles of 64 columns: sizes are bounded after rounding up to these, or 65536 x 1048575 logits would be exactly 2^32 threads."""
+    n = ctypes.c_size_t()
+    for tokens, width, vocab in ((65536, 32, (1 << 20) - 1), (8192, 32, (1 << 23) - 1), (200, 32, (1 << 28) - 1), ((1 << 24) - 1, 4064, 1)):
+        for dt in (cgx.F32, cgx.F16, cgx.BF16):
+            assert lib.cgx_head_workspace(tokens, width, vocab, dt, 0, ctypes.byref(n)) == SIZE
+            assert lib.cgx_head_loss(P, P, P, tokens, width, vocab, dt, -100, P, P, P, 1 << 60, None) == SIZE
+            assert lib.cgx_head_loss_grad(P, P, P, P, P, tokens, width, vocab, dt, -100, P, P, P, 1 << 60, None) == SIZE
+    for tokens, width, vocab in ((65536, 32, (1 << 20) - 64), (8192, 32, (1 << 23) - 64), (200, 32, (1 << 28) - 64), ((1 << 24) - 1, 4032, 1)):
+        assert lib.cgx_head_workspace(tokens, width, vocab, 0, 0, ctypes.byref(n)) == OK
+
+
+def test_head_limits_are_the_documented_ones(tmp_path):
+    """head_layout's answer on sizes around every limit, under the host's sanitizers."""
+    import shutil
+    import subprocess
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "driver")
+    subprocess.run(["g++", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-g", "-O1", "-std=c++17",
+                    os.path.join(here, "host_sanitize", "head_sizes.cpp"),
+                    os.path.join(os.path.dirname(here), "paper_2111_08617_amd", "csrc", "cgx_head.cpp"), "-o", exe], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "all checks passed" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
+    taken, refused = (int(w) for w in run.stdout.split() if w.isdigit())
+    assert taken > 5000 and refused > 5000
