@@ -633,10 +633,24 @@ _HEAD_TYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF1
 _TORCH_NAMES = {F32: "float32", F16: "float16", BF16: "bfloat16"}
 
 
+def _held(v: int, bits: int) -> int:
+    """v, or the end of a signed C type that it lies beyond.  ctypes would cut it down to its low bits, which may well be a size that the
+    library takes; its range's ends are none."""
+    most = (1 << (bits - 1)) - 1
+    return v if -most <= v <= most else most if v > 0 else -most
+
+
+def _mark(name: str, ignore: int) -> int:
+    if not -1 << 63 <= ignore < 1 << 63:
+        raise ValueError(f"{name}: ignore: {ignore} is no int64, so it can mark no target")
+    return ignore
+
+
 def cgx_head_workspace(tokens: int, width: int, vocab: int, dt: int, grad: bool = False) -> int:
     """Bytes of device workspace cgx_head_loss needs; with grad, cgx_head_loss_grad as well."""
     nbytes = ctypes.c_size_t()
-    _check(lib().cgx_head_workspace(tokens, width, vocab, dt, int(bool(grad)), ctypes.byref(nbytes)), "cgx_head_workspace")
+    _check(lib().cgx_head_workspace(_held(tokens, 64), _held(width, 32), _held(vocab, 64), _held(dt, 32), int(bool(grad)),
+                                    ctypes.byref(nbytes)), "cgx_head_workspace")
     return int(nbytes.value)
 
 
@@ -667,8 +681,8 @@ def cgx_head_loss(hidden, weight, targets, loss, lse, workspace, ignore: int = -
     tokens, width, vocab, dt, h, w, t = _head(name, hidden, weight, targets)
     out, sums = (_device_buffer(x, (name, what), tokens * 4, "float32") for x, what in ((loss, "loss"), (lse, "lse")))
     ws = _device_buffer(workspace, (name, "workspace"), 0)              # its size travels with the call: the library checks it
-    _check(lib().cgx_head_loss(h, w, t, tokens, width, vocab, dt, ignore, out, sums, ws, workspace.numel() * workspace.element_size(),
-                               _stream(stream)), name)
+    _check(lib().cgx_head_loss(h, w, t, tokens, _held(width, 32), vocab, dt, _mark(name, ignore), out, sums, ws,
+                               workspace.numel() * workspace.element_size(), _stream(stream)), name)
 
 
 def cgx_head_loss_grad(hidden, weight, targets, lse, dloss, dhidden, dweight, workspace, ignore: int = -100, stream=None) -> None:
@@ -682,7 +696,7 @@ def cgx_head_loss_grad(hidden, weight, targets, lse, dloss, dhidden, dweight, wo
     dh = _device_buffer(dhidden, (name, "dhidden"), tokens * width * size, _TORCH_NAMES[dt])
     dw = _device_buffer(dweight, (name, "dweight"), vocab * width * size, _TORCH_NAMES[dt])
     ws = _device_buffer(workspace, (name, "workspace"), 0)
-    _check(lib().cgx_head_loss_grad(h, w, t, sums, factors, tokens, width, vocab, dt, ignore, dh, dw, ws,
+    _check(lib().cgx_head_loss_grad(h, w, t, sums, factors, tokens, _held(width, 32), vocab, dt, _mark(name, ignore), dh, dw, ws,
                                     workspace.numel() * workspace.element_size(), _stream(stream)), name)
 
 

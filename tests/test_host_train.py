@@ -221,3 +221,50 @@ def test_head_limits_are_the_documented_ones(tmp_path):
     assert run.returncode == 0 and "all checks passed" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
     taken, refused = (int(w) for w in run.stdout.split() if w.isdigit())
     assert taken > 5000 and refused > 5000
+
+
+def test_sizes_and_marks_that_the_c_types_cannot_hold(lib):
+    """ctypes cuts an integer down to its argument's bits without a word: a width of 2^32 + 64 would be one of 64, an ignore mark of
+    2^64 - 100 would be -100."""
+    import torch
+
+    class Fake:
+        is_cuda, device, ndim = True, "cuda:0", 2
+
+        def __init__(self, shape, dtype=torch.float32):
+            self.shape, self.dtype, self.ndim = shape, dtype, len(shape)
+
+        def numel(self): return int(np.prod([int(n) for n in self.shape], dtype=object))
+        def element_size(self): return torch.empty(0, dtype=self.dtype).element_size()
+        def is_contiguous(self): return True
+        def data_ptr(self): return P
+
+    for width in ((1 << 32) + 64, (1 << 31) + 64, -(1 << 32) + 64, 1 << 64):
+        with pytest.raises(cgx.CgxError) as e:
+            cgx.cgx_head_workspace(1, width, 100, cgx.F32)
+        assert e.value.status == SIZE
+    for tokens, vocab in (((1 << 64) + 1, 100), (1, (1 << 64) + 100), (1, -(1 << 64) + 100)):
+        with pytest.raises(cgx.CgxError) as e:
+            cgx.cgx_head_workspace(tokens, 64, vocab, cgx.F32)
+        assert e.value.status == SIZE
+    for dt in ((1 << 32), (1 << 32) + 2, -(1 << 32)):
+        with pytest.raises(cgx.CgxError) as e:
+            cgx.cgx_head_workspace(1, 64, 100, dt)
+        assert e.value.status == DTYPE
+    wide = (1 << 32) + 64
+    args = dict(hidden=Fake((1, wide)), weight=Fake((100, wide)), targets=Fake((1,), torch.int64), lse=Fake((1,)), workspace=Fake((1 << 30,), torch.uint8))
+    with pytest.raises(cgx.CgxError) as e:
+        cgx.cgx_head_loss(**args, loss=Fake((1,)), stream=0)
+    assert e.value.status == SIZE
+    with pytest.raises(cgx.CgxError) as e:
+        cgx.cgx_head_loss_grad(**args, dloss=Fake((1,)), dhidden=Fake((1, wide)), dweight=Fake((100, wide)), stream=0)
+    assert e.value.status == SIZE
+    args.update(hidden=Fake((1, 64)), weight=Fake((100, 64)), workspace=Fake((8,), torch.uint8))
+    for mark in ((1 << 64) - 100, 1 << 63, -(1 << 63) - 1):
+        with pytest.raises(ValueError, match="ignore"):
+            cgx.cgx_head_loss(**args, loss=Fake((1,)), ignore=mark, stream=0)
+        with pytest.raises(ValueError, match="ignore"):
+            cgx.cgx_head_loss_grad(**args, dloss=Fake((1,)), dhidden=Fake((1, 64)), dweight=Fake((100, 64)), ignore=mark, stream=0)
+    for mark in (-(1 << 63), (1 << 63) - 1):                 # these are int64 targets: the workspace is what is refused
+        with pytest.raises(cgx.CgxError):
+            cgx.cgx_head_loss(**args, loss=Fake((1,)), ignore=mark, stream=0)
