@@ -366,3 +366,20 @@ def test_a_factor_that_is_not_finite_stays_its_tokens(torch, size, bad, dtype):
     got = call(torch, hidden, weight, targets, dloss)
     assert torch.equal(got["dhidden"][others], want["dhidden"][others])
     assert not got["dhidden"][at].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("counts", ["all", "two in three"])
+@pytest.mark.parametrize("width", [24, 64, 192])
+def test_several_pieces_of_weights_as_they_lie_and_of_padded_ones(torch, width, counts, dtype):
+    """Rows of whole steps are read where they lie, piece by piece; hidden states too where every token counts and the tokens are whole steps."""
+    tokens, vocab = 16384, 20011 if dtype == "f32" else 34001
+    size = 4 if dtype == "f32" else 2
+    hidden, weight, targets = inputs(torch, tokens, width, vocab, dtype, seed=width)
+    # a piece has a multiple of 256 columns: d of two pieces would not fit the workspace, and no such number divides the vocabulary
+    need = cgx.cgx_head_workspace(tokens, width, vocab, TYPES[dtype], True)
+    assert need < tokens * vocab * size and vocab % 256
+    targets[0], targets[1], targets[2] = vocab - 1, 0, vocab // 2
+    if counts != "all":
+        targets[::3] = -100
+    check(torch, hidden, weight, targets, torch.linspace(-1.0, 1.0, tokens, device="cuda"))
