@@ -220,3 +220,48 @@ def test_lengths_around_an_items_and_lists_around_a_launchs(torch, odd):
         cgx.cgx_grad_clip(grads, norm, max_norm)
         torch.cuda.synchronize()
         assert all(same_bits(torch, g, w) for g, w in zip(grads, in_place))
+
+
+def test_lists_beyond_the_memory_side_cache(torch):
+    """More than 256 MB of gradients of three types, each starting at an odd element: the norm's loads and the clipping's stores past the
+    caches, in place and into a fused buffer of each type (230 MB and more).  The results are formed on the device, by the same binary32
+    arithmetic that torch's elementwise operations are."""
+    sizes = [(33 << 20) + 5, (49 << 20) + 1, (37 << 20) + 3, 4097, 0, 7]
+    kinds = ("f32", "bf16", "f16")
+
+    def fresh():
+        g = torch.Generator(device="cuda").manual_seed(31)
+        out = []
+        for k, n in enumerate(sizes):
+            buf = torch.full((n + 16,), 11.0, dtype={"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[kinds[k % 3]], device="cuda")
+            part = buf[2 * k + 1:2 * k + 1 + n]
+            part.copy_(torch.randn(n, generator=g, device="cuda") * 10.0 ** -(k % 3))
+            out.append(part)
+        return out
+
+    def bits(t):
+        return t.view(torch.int32 if t.dtype == torch.float32 else torch.int16)
+
+    grads = fresh()
+    assert sum(g.numel() * g.element_size() for g in grads) > 256 << 20
+    want = math.sqrt(math.fsum(float(part.double().square().sum()) for g in grads for part in g.split(1 << 24)))
+    norm = norm_of(torch, grads)
+    assert abs(float(norm) - want) <= 2.0**-23 * want
+    assert torch.equal(norm, norm_of(torch, grads)), "not the same bits again"
+    max_norm = float(np.float32(want / 3))
+    factor = (torch.tensor([max_norm], dtype=torch.float32) / norm.cpu()).cuda()
+    total = sum(sizes)
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        fused = torch.full((total + 64,), -7.0, dtype=dtype, device="cuda")
+        assert total * fused.element_size() > 128 << 20
+        cgx.cgx_grad_clip(grads, norm, max_norm, out=fused)
+        at = 0
+        for g in grads:
+            assert torch.equal(bits(fused[at:at + g.numel()]), bits((g.float() * factor).to(dtype)))
+            at += g.numel()
+        assert (fused[total:] == -7.0).all()
+    cgx.cgx_grad_clip(grads, norm, max_norm)
+    for g, before in zip(grads, fresh()):
+        assert torch.equal(bits(g), bits((before.float() * factor).to(before.dtype)))
+        around = torch.cat([g.as_strided((g.storage_offset(),), (1,), 0), g.as_strided((16 - g.storage_offset(),), (1,), g.storage_offset() + g.numel())])
+        assert (around == 11.0).all(), "wrote beside a tensor"
