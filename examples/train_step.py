@@ -6,11 +6,15 @@ The model predicts the next token from the current one: an embedding, a mixing m
 differentiates the two layers in front; everything from the hidden states on runs in this library's kernels:
 
   cgx_head_loss, cgx_head_loss_grad   the loss over the vocabulary and its gradients, without the logits
-  cgx_grad_norm, cgx_grad_clip        the gradients of all layers, clipped by their global norm into one fused buffer
+  cgx_grad_clip                       (with no limit yet) the gradients of all layers, converted into one fused buffer
   cgx_quantize                        that buffer, compressed layer by layer: what the rank would send
+  cgx_dequantize                      the gradient that every rank holds after the exchange (here there is one rank)
+  cgx_grad_norm, cgx_grad_clip        its norm, and its clipping in place
 
-Then the update is made from the compressed gradients (cgx_dequantize), as every rank makes it after the exchange.
+The norm is that of the exchanged gradient, so all ranks clip by the same factor.  Clipping a rank's own gradients ahead of the exchange
+would give each rank a factor of its own, and the step another direction.
 """
+import math
 import os
 import sys
 
@@ -46,7 +50,7 @@ class Model:
         self.workspace = torch.empty(cgx.cgx_head_workspace(BATCH, WIDTH, VOCAB, cgx.BF16, grad=True), dtype=torch.uint8, device="cuda")
         self.norm_workspace = torch.empty(cgx.cgx_grad_norm_workspace(), dtype=torch.uint8, device="cuda")
         self.loss, self.lse = torch.empty(BATCH, device="cuda"), torch.empty(BATCH, device="cuda")
-        self.norm = torch.empty(1, device="cuda")
+        self.norm, self.zero = torch.empty(1, device="cuda"), torch.zeros(1, device="cuda")
 
     def gradients(self, tokens, targets):
         """(mean loss, gradients of the layers) of one batch; targets may hold IGNORE."""
@@ -63,10 +67,12 @@ class Model:
 
     def step(self, tokens, targets, seed: int, rate: float = 2.0, max_norm: float = 1.0):
         loss, grads = self.gradients(tokens, targets)
-        cgx.cgx_grad_norm(grads, self.norm, self.norm_workspace)
-        cgx.cgx_grad_clip(grads, self.norm, max_norm, out=self.fused)
+        cgx.cgx_grad_clip(grads, self.zero, math.inf, out=self.fused)
         cgx.cgx_quantize(self.fused, self.plan, seed, self.packed, self.meta)
+        # (ranks would exchange their chunks here, and average them)
         cgx.cgx_dequantize(self.packed, self.meta, self.plan, cgx.F32, self.fused)
+        cgx.cgx_grad_norm([self.fused], self.norm, self.norm_workspace)
+        cgx.cgx_grad_clip([self.fused], self.norm, max_norm)
         with torch.no_grad():
             for p, lo, hi in zip(self.layers, self.plan.offsets[:-1], self.plan.offsets[1:]):
                 p -= rate * self.fused[lo:hi].view_as(p)

@@ -393,10 +393,11 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
                                  int32_t *buckets_out /* host [L] */);
 
 /*
- * What stands in front of the fused buffer in a language model's training step: the loss over the
- * vocabulary, whose weight is the largest layer of every Transformer plan, and the clipping of all
- * gradients by their global norm.  These calls take no plan; they allocate nothing, copy nothing from
- * the host on the stream, and may be captured into a graph.
+ * What a language model's training step does beside the compression: the loss over the vocabulary,
+ * whose weight is the largest layer of every Transformer plan, in front of the fused buffer; and the
+ * clipping of gradients by their global norm, behind the exchange, or into the fused buffer.  These
+ * calls take no plan; they allocate nothing, copy nothing from the host on the stream, and may be
+ * captured into a graph.
  *
  * Softmax cross entropy of a head (the last matrix product of a language model) without its logits.
  *   z[n][v] = sum_h hidden[n][h] * weight[v][h]
@@ -451,6 +452,10 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  *   workspace  device, 16-byte aligned, at least the bytes cgx_grad_norm_workspace reports (CGX_ERR_SIZE
  *              otherwise).  Calls that share one must not overlap.
  * A launch covers up to 240 tensors; longer lists take more.
+ * In a data-parallel step the norm to clip by is that of the exchanged gradient: both calls then take the
+ * decompressed buffer, a list of one tensor, and scale it in place, by the same factor on every rank.  Clipping
+ * a rank's own gradients ahead of the exchange is another algorithm, with a factor of its own on each rank.
+ * With an infinite max_norm cgx_grad_clip scales nothing (unless norm is NaN): it converts and fuses.
  */
 typedef struct {
     void *data;       /* device */

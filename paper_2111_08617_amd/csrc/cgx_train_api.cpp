@@ -1,4 +1,4 @@
-// extern "C" entry points of what stands in front of the fused buffer (see include/cgx.h): the head's loss and its gradient,
+// extern "C" entry points of what stands beside the fused buffer (see include/cgx.h): the head's loss and its gradient,
 // the gradients' norm and clipping.  Argument checks, then launches on the caller's stream.
 #include <hip/hip_runtime.h>
 

@@ -39,3 +39,18 @@ def test_gradients_of_the_step(example):
 def test_the_step_learns_from_clipped_compressed_gradients(example):
     losses = example.main(steps=60)
     assert losses[0] > 7.0 and losses[-1] < 0.7 * losses[0]
+
+
+def test_the_step_clips_the_exchanged_gradient(example):
+    """What the update takes has the limit's norm: clipping comes after the exchange, which changes norms (rounding to 8 bits adds to them),
+    and its factor follows from what every rank holds.  Limit / norm, the norm itself and the products are each rounded to binary32."""
+    import torch
+    model = example.Model(seed=3)
+    for max_norm in (0.05, 1e9):
+        before = [p.detach().clone() for p in model.layers]
+        model.step(*example.batch(0), seed=1, rate=1.0, max_norm=max_norm)
+        size, norm = float(model.fused.double().norm()), float(model.norm)
+        assert norm > 0.05
+        assert abs(size - min(max_norm, norm)) <= 2.0**-22 * size
+        for p, b, lo, hi in zip(model.layers, before, model.plan.offsets[:-1], model.plan.offsets[1:]):
+            assert torch.equal(p.detach(), b - model.fused[lo:hi].view_as(b))

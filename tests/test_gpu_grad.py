@@ -265,3 +265,15 @@ def test_lists_beyond_the_memory_side_cache(torch):
         assert torch.equal(bits(g), bits((before.float() * factor).to(before.dtype)))
         around = torch.cat([g.as_strided((g.storage_offset(),), (1,), 0), g.as_strided((16 - g.storage_offset(),), (1,), g.storage_offset() + g.numel())])
         assert (around == 11.0).all(), "wrote beside a tensor"
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_an_infinite_limit_converts_and_fuses(torch, out):
+    grads = tensors(torch, [5000, 0, 4097, 33], ("f32", "bf16", "f16"), seed=8)
+    dtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[out]
+    for norm in (0.0, 3.0, math.inf):
+        fused = torch.full((9130 + 64,), -7.0, dtype=dtype, device="cuda")
+        cgx.cgx_grad_clip(grads, torch.tensor([norm], device="cuda"), math.inf, out=fused)
+        assert same_bits(torch, fused[:9130], torch.cat([g.to(dtype) for g in grads])) and (fused[9130:] == -7.0).all()
+    cgx.cgx_grad_clip(grads, torch.tensor([math.nan], device="cuda"), math.inf, out=fused)
+    assert fused[:9130].isnan().all()
