@@ -407,9 +407,11 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
  *   d[n][v]       = dloss[n] * (exp(z[n][v] - lse[n]) - (v == targets[n]))
  *   dhidden[n][h] = sum_v d[n][v] * weight[v][h],  dweight[v][h] = sum_n d[n][v] * hidden[n][h]
  * Logits are formed tile by tile and kept by neither call; the second one forms them again, holds d for a
- * piece of the vocabulary at a time in the workspace, in the type of the operands (16-bit types: in units of
- * the largest dloss, which keeps it in range).  Products are summed in binary32, each result is rounded once.
- * The order of every sum is fixed: the same call gives the same bits again.
+ * piece of the vocabulary at a time in the workspace, rounded to the type of the operands (16-bit types: in
+ * units of the largest finite dloss, which keeps it in range; in binary16 an element of d below 2^-28 of that
+ * loses bits and one below 2^-39 is lost).  Products are summed in binary32, each result is rounded once.
+ * The order of every sum is fixed: the same call gives the same bits again.  A logit that is NaN or +infinity
+ * makes its token's loss and lse NaN.
  *   hidden    device, tokens x width elements of dt (CGX_F32, CGX_F16 or CGX_BF16), dense
  *   weight    device, vocab x width elements of dt, dense
  *   targets   device, tokens int64 (8-byte aligned).  A token whose target is `ignore` has loss and lse 0
@@ -420,6 +422,7 @@ int cgx_assign_buckets_from_bits(int32_t L, const uint8_t *bits_per_layer /* hos
  *   dhidden, dweight   device, tokens x width and vocab x width elements of dt; every element is written
  *   workspace device, 16-byte aligned, at least the bytes cgx_head_workspace reports (CGX_ERR_SIZE
  *             otherwise); contents unspecified before and after.  Calls that share one must not overlap.
+ *             For gradients at least 134 MB: two sections for the partial sums of a whole chip's tiles.
  * Outputs overlap no input.  tokens may be 0 (dweight is then zero); 0 <= tokens < 2^24, 1 <= width <= 2^17, 1 <= vocab,
  * and the tokens, rounded up to a multiple of 256 (one at least), times vocab or times width, both rounded up to a multiple
  * of 64, below 2^36, so that a launch can hold them: vocab <= 2^28 - 64 for up to 256 tokens (CGX_ERR_SIZE otherwise).

@@ -189,8 +189,9 @@ __device__ __forceinline__ void scale_item(const void *src, int64_t from, void *
 }
 
 // x * factor, in place (OUT < 0: each tensor in its own type) or into the fused buffer.  factor = min(1, max_norm / norm) in binary32;
-// the product is rounded once, to the result's type.  2.2 GB of bfloat16 into 4.4 GB of binary32: 1128 us (5.8 TB/s; a copy of 4 GB
-// by the library 4.75); 102 MB of binary32, which the norm has left in the memory-side cache, 31 us (6.5 TB/s).
+// the product is rounded once, to the result's type.  2.2 GB of bfloat16 into 4.4 GB of binary32: 1120 us (5.9 TB/s; a copy of 4 GB
+// by the library 4.75); 102 MB of binary32, which the norm has left in the memory-side cache, 31 us (6.6 TB/s).  In place, 5.3 GB of binary32:
+// 1890 us (5.6 TB/s).
 template <int OUT, bool STREAM>
 __global__ __launch_bounds__(kBlock) void clip_items(Group group, const float *norm, float max_norm, void *out)
 {

@@ -160,8 +160,9 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
     const Totals t = block_totals(mine, totals);
     // d is held in units of the largest factor, times 2^top_bits.  With factors that are all alike (a mean over tokens) a target that has
     // no probability yet then is exactly -2^top_bits, and near 1 the rounding is at its finest: in units of 1 all targets of a call
-    // would be off by the same rounding of the factor, and with them the whole gradient, by up to 2^-8.  In binary16, with 14, probabilities down to
-    // 1e-9 stay normal numbers and nothing overflows, whatever the loss scale.
+    // would be off by the same rounding of the factor, and with them the whole gradient, by up to 2^-8.  In binary16, with 14, elements of d down to
+    // 2^-28 (4e-9) of the largest factor stay normal numbers, those under 2^-39 are lost, and nothing overflows, whatever the loss scale: a token
+    // whose factor is far below the largest one keeps fewer of its small probabilities.
     // A factor that is not finite makes its own token's d so; the unit comes from the others, whose dhidden is none the worse for it.
     const float unit = !top_bits || t.top == 0.f ? 1.f : fmaxf(t.top, 0x1p-100f);
     if (blockIdx.x == 0 && tid == 0) *header = Header{t.all, ldexpf(unit, -top_bits)};
@@ -246,9 +247,11 @@ using Lds = unsigned char[K::kLds];
 // Logits of a tile, and what its rows add to their softmax: the largest logit m, the sum of exp(logit - m), in binary32; parts join by
 // m = max m_k, sum = sum_k sum_k exp(m_k - m), so that no logit is ever stored.  A lane holds 16 neighbouring columns of a row (strips),
 // so a row's maximum and sum take two exchanges between lanes and one between waves.
-// Bound by the matrix cores: 8192 x 2048 x 50257 bfloat16 1266 us = 1.33 PFLOP/s (library products of the same shapes: 1.07 to 1.37), which
-// issue in 0.63 of the cycles; without exponentials, maxima and stores it takes 0.95 of that time.  binary32, 509 x 768 x 30522: 184 us =
-// 130 TFLOP/s of 154.  With few tokens by reading W: 32 x 2048 x 50257 34 us from the memory-side cache, about 50 from memory.
+// Bound by the matrix cores: 8192 x 2048 x 50257 bfloat16 1290 us = 1.31 PFLOP/s (the library's product of this shape 1.23), which
+// issue in 0.63 of the cycles; without exponentials, maxima and stores it takes 0.95 of that time.  Sixteen steps per tile leave more of its
+// ends uncovered: 4096 x 1024 x 50257 binary16 419 us = 1.01 PFLOP/s (the library's 0.86).  binary32, 509 x 768 x 30522: 205 us =
+// 117 TFLOP/s of 154 in single passes, 180 us back to back.  With few tokens by reading W: 32 x 2048 x 50257 34 us from the memory-side cache,
+// about 50 from memory.
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                           int64_t pitch, int64_t first, int64_t columns, int64_t parts,
@@ -499,9 +502,12 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tok
 // d of a tile of a piece: logits as above, then dloss (exp(z - lse) - [v = target]) in its units, in the operands' type.
 // Every element of the piece's whole tiles is written; those of no token or no column are zeros.
 // d is rounded to the operands' type once, because the products that follow read it from the matrix cores' operands: its relative error,
-// half a unit of that type, is what the results are rounded to as well.  Forming the logits again costs 2 N V H operations and saves 4 N V
-// bytes written and read by the loss and N V bytes of workspace that would have to live from one call to the other.
-// 8192 tokens x 2048 x 25344 columns, bfloat16: 704 us = 1.21 PFLOP/s, with 0.41 GB written at the tiles' ends while no products run.
+// half a unit of that type, is what the results are rounded to as well.  Gradients of partly trained heads (8192 and 4096 tokens before 30522 and
+// 50257 columns) are 1.07 to 1.11 times as far from the exact ones as these rounded to bfloat16, 1.17 times in binary16, all of it from the
+// one element of a row that is its target's; d in two parts would take that away for 4 N V H more operations.
+// Forming the logits again costs 2 N V H operations and saves 4 N V bytes written and read by the loss and N V bytes of workspace that would have
+// to live from one call to the other.
+// 8192 tokens x 2048 x 25344 columns, bfloat16: 709 us = 1.20 PFLOP/s, with 0.41 GB written at the tiles' ends while no products run.
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                            int64_t pitch, int64_t first, int64_t columns,
@@ -581,7 +587,7 @@ __device__ __forceinline__ f32x4 joined(const float *first, int64_t apart, uint3
 }
 
 // dx += d W over a piece, in binary32.  accumulate: not the first piece.  W is read along its rows, as stored; the matrix cores want its
-// columns, and transposing LDS reads give them (Side::fragment).  8192 x 25344 columns x 2048, bfloat16: 612 us = 1.39 PFLOP/s.
+// columns, and transposing LDS reads give them (Side::fragment).  8192 x 25344 columns x 2048, bfloat16: 616 us = 1.38 PFLOP/s.
 template <typename K>
 __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *header, const typename K::T *delta, int64_t piece,
                                                             const typename K::T *weight, int64_t pitch, int64_t columns, int32_t blocks,
@@ -624,7 +630,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
 // dW = d^T x for the rows of a piece.  The tiles fill the chip's compute units some number of times; those of the last, partial round are
 // split over the tokens into as many parts as fill it, each part with sums of its own (`spare`, by part and tile), which weight_rest
 // joins.  (Without that, 50257 x 2048 weights in two pieces took 4 rounds each for 3.06 rounds' work.)  Both operands are read along their
-// rows and transposed on their way out of LDS.  25344 rows, 8192 tokens, width 2048, bfloat16: 640 us = 1.33 PFLOP/s, and 11 us of joining.
+// rows and transposed on their way out of LDS.  25344 rows, 8192 tokens, width 2048, bfloat16: 653 us = 1.30 PFLOP/s, and 11 us of joining.
 struct Rounds {
     uint32_t whole;          // tiles that a block computes alone
     uint32_t rest;           // tiles of the last round
@@ -731,7 +737,8 @@ __global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t
 }
 
 // dhidden from the sums, in their units; a block per token.  side, steps: of the kernel that left them.  Bound by memory: 8192 x 2048
-// binary32 sums to bfloat16 23 us (101 MB, 4.4 TB/s); 4096 tokens of 768, the 15 % that count in seven parts, 12 us.
+// binary32 sums to bfloat16 23 us (101 MB, 4.4 TB/s); 4096 tokens of 768, the 15 % that
+// count in 28 parts (their nine tiles, over 256 compute units: 53 MB), 12.5 us.
 template <typename T>
 __global__ __launch_bounds__(256) void round_hidden(const Header *header, const int32_t *__restrict__ place, const float *__restrict__ sums,
                                                     int64_t pitch, int64_t width, int32_t side, int32_t steps, int32_t blocks,

@@ -56,7 +56,8 @@ enum Layout {
 
 // 16 bytes per lane from base + offset (base uniform) to LDS, lane l's at address dst + 16 l (dst uniform).  Written out because the compiler,
 // which cannot tell apart the stage that such a load fills and the one that a transposing LDS read takes, makes every such read wait for all
-// loads that the builtin has issued; the waits that are needed are in Tile.
+// loads that the builtin has issued; the waits that are needed are in Tile.  (The compiler keeps m0 for itself, so no clobber may name it; it sets it
+// just ahead of what needs it, and nothing else in these kernels does.)
 __device__ __forceinline__ void to_lds(const void *base, uint32_t offset, uint32_t dst)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
