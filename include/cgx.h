@@ -438,6 +438,30 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
                        void *stream);
 
 /*
+ * Embedding: rows of a table for a list of tokens, and the table's gradient.
+ *   cgx_embed       out[n][h] = scale * table[ids[n]][h]
+ *   cgx_embed_grad  dtable[v][h] = scale * sum_{n: ids[n] = v} dout[n][h]  (+ dtable[v][h] with accumulate)
+ * Products and sums in binary32, rounded once to the type of the result.  The gradient's tokens are sorted by id, and the order of every sum is
+ * fixed by the ids: the same call gives the same bits again.  With accumulate, rows of no token are neither read nor written: a table that is
+ * also the head's weight has its two gradients added by cgx_head_loss_grad, which writes all of dweight, and this call on the same buffer behind it.
+ *   table, dtable   device, vocab x width elements of dt (CGX_F32, CGX_F16 or CGX_BF16), dense.  Without accumulate every element of dtable
+ *                   is written; rows of no token are zeros.
+ *   ids       device, tokens int64 (8-byte aligned), repeated as they come.  A token whose id is `ignore` (padding; it may be an entry of the
+ *             vocabulary) has a row of zeros in out and takes no part in dtable, whatever its row of dout holds.  Any other id outside [0, vocab)
+ *             makes its row of out NaN, and has no row in dtable.
+ *   out, dout device, tokens x width elements of dt, dense; every element of out is written
+ *   workspace device, 16-byte aligned, at least the bytes cgx_embed_grad_workspace reports (CGX_ERR_SIZE otherwise); contents unspecified before
+ *             and after.  Calls that share one must not overlap.
+ * Outputs overlap no input.  tokens may be 0; 0 <= tokens < 2^24, 1 <= width <= 2^17, 1 <= vocab < 2^28, and both tokens and vocab
+ * times width below 2^35 (CGX_ERR_SIZE otherwise).
+ */
+int cgx_embed(const void *table, const int64_t *ids, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, int64_t ignore, float scale,
+              void *out, void *stream);
+int cgx_embed_grad_workspace(int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, size_t *bytes);
+int cgx_embed_grad(const void *dout, const int64_t *ids, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, int64_t ignore, float scale,
+                   int32_t accumulate, void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Global l2 norm of a list of gradient tensors, and their clipping by it.
  *   norm   = sqrt(sum over all tensors and elements of x^2), summed in binary64 in a fixed order, rounded to
  *            binary32 at the end

@@ -33,6 +33,7 @@ EXPORTS = ("cgx_sizes", "cgx_quantize", "cgx_dequant_reduce", "cgx_dequant_reduc
            "cgx_qsgd_layered_quantize", "cgx_qsgd_layered_dequant_reduce", "cgx_qsgd_layered_dequant_reduce_requantize",
            "cgx_plan_tiles", "cgx_plan_tiles_chunk", "cgx_stream_probe", "cgx_stream_probe_shaped",
            "cgx_issue_probe", "cgx_issue_probe_form", "cgx_head_workspace", "cgx_head_loss", "cgx_head_loss_grad",
+           "cgx_embed", "cgx_embed_grad_workspace", "cgx_embed_grad",
            "cgx_grad_norm_workspace", "cgx_grad_norm", "cgx_grad_clip", "cgx_status_string", "cgx_shutdown")
 
 TILE_DTYPE = np.dtype([("elem0", "<i8"), ("packed_off", "<i8"), ("bucket0", "<u4"), ("count", "<u4"),
@@ -116,6 +117,10 @@ def lib() -> ctypes.CDLL:
                                     c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
         L.cgx_head_loss_grad.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64,
                                          c.c_int, c.c_int64, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.cgx_embed.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int64, c.c_float, c.c_void_p, c.c_void_p]
+        L.cgx_embed_grad_workspace.argtypes = [c.c_int64, c.c_int32, c.c_int64, c.c_int, c.POINTER(c.c_size_t)]
+        L.cgx_embed_grad.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int64, c.c_float, c.c_int32,
+                                     c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
         L.cgx_grad_norm_workspace.argtypes = [c.POINTER(c.c_size_t)]
         L.cgx_grad_norm.argtypes = [c.c_void_p, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
         L.cgx_grad_clip.argtypes = [c.c_void_p, c.c_int32, c.c_void_p, c.c_float, c.c_void_p, c.c_int, c.c_void_p]
@@ -698,6 +703,63 @@ def cgx_head_loss_grad(hidden, weight, targets, lse, dloss, dhidden, dweight, wo
     ws = _device_buffer(workspace, (name, "workspace"), 0)
     _check(lib().cgx_head_loss_grad(h, w, t, sums, factors, tokens, _held(width, 32), vocab, dt, _mark(name, ignore), dh, dw, ws,
                                     workspace.numel() * workspace.element_size(), _stream(stream)), name)
+
+
+def _here(name: str, stream, *tensors) -> int:
+    """The stream of a call, which runs on the current device: tensors of another one are refused."""
+    import torch
+    device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    for t, what in tensors:
+        if t.get_device() != device:
+            raise ValueError(f"{name}: {what}: the tensor lives on {t.device}, the call runs on the current device, cuda:{device}")
+    return _stream(stream)
+
+
+def _embedding(name: str, table, what: str, ids, rows, across: str):
+    """(tokens, width, vocab, dt, addresses of the table, ids and rows) of an embedding's call."""
+    for t, w in ((table, what), (rows, across)):
+        if getattr(t, "ndim", 0) != 2:
+            raise ValueError(f"{name}: {w}: a matrix is needed, a row for each {'entry of the vocabulary' if t is table else 'token'}")
+    (vocab, width), (tokens, wide) = table.shape, rows.shape
+    dt = _HEAD_TYPES.get(str(table.dtype))
+    if dt is None:
+        raise ValueError(f"{name}: {what}: element type {table.dtype}, expected torch.float32, torch.float16 or torch.bfloat16")
+    if wide != width:
+        raise ValueError(f"{name}: {across}: rows of {wide} elements, those of {what} have {width}")
+    if ids.numel() != tokens:
+        raise ValueError(f"{name}: ids: {ids.numel()} entries for {tokens} rows of {across}")
+    size = 4 if dt == F32 else 2
+    return (tokens, _held(width, 32), vocab, dt, _device_buffer(table, (name, what), vocab * width * size, _TORCH_NAMES[dt]),
+            _device_buffer(ids, (name, "ids"), tokens * 8, "int64"), _device_buffer(rows, (name, across), tokens * width * size, _TORCH_NAMES[dt]))
+
+
+def cgx_embed(table, ids, out, scale: float = 1.0, ignore: int = -100, stream=None) -> None:
+    """out[n] = scale * table[ids[n]].  table: [vocab, width], out: [tokens, width] of one type (float32, float16, bfloat16); ids:
+    int64[tokens] (of any shape with as many entries), `ignore` marks tokens whose row is zeros."""
+    name = "cgx_embed"
+    tokens, width, vocab, dt, t, i, o = _embedding(name, table, "table", ids, out, "out")
+    _check(lib().cgx_embed(t, i, tokens, width, vocab, dt, _mark(name, ignore), float(scale), o,
+                           _here(name, stream, (table, "table"), (ids, "ids"), (out, "out"))), name)
+
+
+def cgx_embed_grad_workspace(tokens: int, width: int, vocab: int, dt: int) -> int:
+    """Bytes of device workspace cgx_embed_grad needs."""
+    nbytes = ctypes.c_size_t()
+    _check(lib().cgx_embed_grad_workspace(_held(tokens, 64), _held(width, 32), _held(vocab, 64), _held(dt, 32), ctypes.byref(nbytes)),
+           "cgx_embed_grad_workspace")
+    return int(nbytes.value)
+
+
+def cgx_embed_grad(dout, ids, dtable, workspace, scale: float = 1.0, ignore: int = -100, accumulate: bool = False, stream=None) -> None:
+    """dtable[v] = scale * the sum of dout[n] over the tokens n with ids[n] == v, zeros where there are none; with accumulate it is added to
+    what dtable holds (the head's gradient of a tied table, or that of an earlier part of the batch).  dout: [tokens, width], dtable:
+    [vocab, width]; workspace: device tensor of cgx_embed_grad_workspace bytes."""
+    name = "cgx_embed_grad"
+    tokens, width, vocab, dt, t, i, d = _embedding(name, dtable, "dtable", ids, dout, "dout")
+    ws = _device_buffer(workspace, (name, "workspace"), 0)
+    _check(lib().cgx_embed_grad(d, i, tokens, width, vocab, dt, _mark(name, ignore), float(scale), int(bool(accumulate)), t, ws,
+                                workspace.numel() * workspace.element_size(),
+                                _here(name, stream, (dout, "dout"), (ids, "ids"), (dtable, "dtable"), (workspace, "workspace"))), name)
 
 
 def cgx_grad_norm_workspace() -> int:

@@ -20,7 +20,8 @@ SOURCES = [("cgx_plan.cpp", "cgx_plan", []), ("cgx_api.cpp", "cgx_api", []), ("c
            ("cgx_fused.hip", "cgx_fused_g4", ["-DCGX_GROUPS=4"]), ("cgx_wide.hip", "cgx_wide", []),
            ("cgx_stats.hip", "cgx_stats", []),
            ("cgx_probe.hip", "cgx_probe", []), ("cgx_train_api.cpp", "cgx_train_api", []), ("cgx_head.cpp", "cgx_head_layout", []),
-           ("cgx_head.hip", "cgx_head", []), ("cgx_grad.hip", "cgx_grad", [])]
+           ("cgx_head.hip", "cgx_head", []), ("cgx_grad.hip", "cgx_grad", []),
+           ("cgx_embed.cpp", "cgx_embed_layout", []), ("cgx_embed.hip", "cgx_embed", [])]
 
 # -ffp-contract=off: the code decision is binary32 without fused operations.
 # packed-fp32 instructions stay disabled for this target.

@@ -1,0 +1,466 @@
+// The embedding's kernels and their launches: rows of a table for a list of tokens, and the table's gradient.
+//
+//   lookup    out[n] = scale table[ids[n]]
+//   gradient  dtable[v] = scale sum_{n: ids[n] = v} dout[n]  (+ dtable[v])
+// Both are bound by memory: an element read or written costs less than one vector instruction.  The gradient's sums are taken in the order of
+// the tokens sorted by id, so that a row is written once, by one wave, and no atomics are needed: the same call gives the same bits.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "cgx_embed.h"
+
+namespace cgx {
+namespace {
+
+constexpr int kBlock = 256;
+
+struct EmbedHeader {
+    int32_t count;           // tokens that take part
+};
+
+// 16 bytes of a row, V elements; rows start at any element.
+template <typename T>
+struct Piece {
+    static constexpr int V = 16 / int(sizeof(T));
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    typedef Vec Anywhere __attribute__((aligned(sizeof(T))));
+    static __device__ __forceinline__ Vec load(const T *row, int64_t column, int64_t width)
+    {
+        if (column + V <= width) return *reinterpret_cast<const Anywhere *>(row + column);
+        Vec v = Vec(T(0.f));
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (column + e < width) v[e] = row[column + e];
+        return v;
+    }
+    static __device__ __forceinline__ void store(T *row, int64_t column, int64_t width, Vec v)
+    {
+        if (column + V <= width) {
+            *reinterpret_cast<Anywhere *>(row + column) = v;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (column + e < width) row[column + e] = v[e];
+    }
+};
+
+// ---------------------------------------------------------------- lookup
+
+// A wave takes EACH strips (of 64 x 16 bytes) of a row, all of them on their way at a time.
+template <typename T, int EACH>
+__global__ __launch_bounds__(kBlock) void look_up(const T *__restrict__ table, const int64_t *__restrict__ ids, int64_t tokens, int64_t width,
+                                                  int64_t vocab, int64_t ignore, float scale, uint32_t parts, T *__restrict__ out)
+{
+    using P = Piece<T>;
+    const int lane = int(threadIdx.x) & 63;
+    const int64_t item = int64_t(blockIdx.x) * (kBlock / 64) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int64_t token = item / parts, first = (item % parts * EACH * 64 + lane) * P::V;
+    if (token >= tokens) return;
+    const int64_t id = ids[token];
+    const bool there = id >= 0 && id < vocab && id != ignore;
+    const float otherwise = id == ignore ? 0.f : __builtin_nanf("");
+    const T *row = table + (there ? id : 0) * width;
+    T *const to = out + token * width;
+    typename P::Vec v[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; k++) {
+        const int64_t column = first + k * 64 * P::V;
+        if (there && column < width) v[k] = P::load(row, column, width);
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; k++) {
+        const int64_t column = first + k * 64 * P::V;
+        if (column >= width) break;
+        typename P::Vec r;
+#pragma unroll
+        for (int e = 0; e < P::V; e++) r[e] = T(there ? float(v[k][e]) * scale : otherwise);
+        P::store(to, column, width, r);
+    }
+}
+
+// ---------------------------------------------------------------- gradient: tokens sorted by id
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortEach = 8, kDigitBits = 8, kDigits = 1 << kDigitBits;
+
+struct SortShared {
+    uint32_t place[kSortWaves][kDigits];     // entries of a digit in a wave's part, then where the next one of them goes
+    uint32_t waves[kSortWaves], all[kSortWaves];
+};
+
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// One stable pass of a sort by digits, by a block: `read(i, key, token)` says whether entry i of n takes part, and `write(place, key, token)`
+// gets the entries in the order of the digit `key >> shift`, those of one digit in the order of i.  `counted(first)` is called by all threads
+// between the two walks over the entries.  Each wave takes a run of neighbouring entries, so that ranks within a digit follow from
+// the counts of the waves before it and, among its own 64 at a time, from votes.
+template <class Read, class Counted, class Write>
+__device__ __forceinline__ void sort_pass(SortShared &s, int64_t n, int shift, int bits, Read read, Counted counted, Write write)
+{
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, from = wave * each, to = from + each < n ? from + each : n;
+    const uint32_t mask = (1u << bits) - 1;
+    for (int k = tid; k < kSortWaves * kDigits; k += kSortThreads) s.place[0][k] = 0;
+    __syncthreads();
+    for (int64_t i = from; i < to; i += 64 * kSortEach) {
+        uint32_t key[kSortEach] = {};
+        int32_t token[kSortEach] = {};
+        bool in[kSortEach];
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++) in[k] = i + 64 * k + lane < to && read(i + 64 * k + lane, key[k], token[k]);
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++)
+            if (in[k]) atomicAdd(&s.place[wave][(key[k] >> shift) & mask], 1u);
+    }
+    __syncthreads();
+    // places: digits in order, the waves of a digit in order
+    uint32_t mine = 0, before = 0;
+    if (tid < kDigits) {
+        for (int w = 0; w < kSortWaves; w++) mine += s.place[w][tid];
+        before = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t other = __shfl_up(before, d, 64);
+            before += lane >= d ? other : 0;
+        }
+        if (lane == 63) s.waves[wave] = before;
+    }
+    __syncthreads();
+    if (tid < kDigits) {
+        before -= mine;
+        for (int w = 0; w < wave; w++) before += s.waves[w];
+        for (int w = 0; w < kSortWaves; w++) {
+            const uint32_t here = s.place[w][tid];
+            s.place[w][tid] = before;
+            before += here;
+        }
+    }
+    counted();
+    __syncthreads();
+    for (int64_t i = from; i < to; i += 64 * kSortEach) {
+        uint32_t key[kSortEach] = {};
+        int32_t token[kSortEach] = {};
+        bool in[kSortEach];
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++) in[k] = i + 64 * k + lane < to && read(i + 64 * k + lane, key[k], token[k]);
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++) {
+            const uint64_t vote = __ballot(in[k]);
+            if (!vote) continue;
+            const uint32_t digit = (key[k] >> shift) & mask;
+            uint64_t same = vote;
+            for (int b = 0; b < bits; b++) {
+                const uint64_t ones = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? ones : ~ones;
+            }
+            if (in[k]) {
+                const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1))), first = s.place[wave][digit];
+                write(first + rank, key[k], token[k]);
+                __builtin_amdgcn_wave_barrier();
+                if (rank == 0) s.place[wave][digit] = first + uint32_t(__popcll(same));
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    }
+    __syncthreads();
+}
+
+struct SortArrays {
+    int32_t *token[2], *id[2];
+};
+
+// The first sort_blocks blocks sort: each looks at all ids for those of its share of the vocabulary, and for how many there are ahead of it, and
+// sorts its own, stably, eight bits of their place in the share at a time (one pass for up to 65536 entries).  The blocks behind them write
+// zeros over the table meanwhile, which hides the sort wherever the table is long.
+constexpr int kFillBytes = 64 << 10;                 // of the table, a block
+template <bool FILL>
+__global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__restrict__ ids, int64_t tokens, int64_t ignore, int64_t vocab,
+                                                            int64_t share, int32_t bits, uint32_t sort_blocks, EmbedHeader *header,
+                                                            SortArrays a, unsigned char *__restrict__ table, int64_t bytes)
+{
+    const int tid = int(threadIdx.x);
+    if (FILL && blockIdx.x >= sort_blocks) {
+        typedef uint32_t Vec __attribute__((ext_vector_type(4)));
+        const int64_t first = int64_t(blockIdx.x - sort_blocks) * kFillBytes;
+#pragma unroll
+        for (int k = 0; k < kFillBytes / (16 * kSortThreads); k++) {
+            const int64_t at = first + (int64_t(k) * kSortThreads + tid) * 16;
+            if (at + 16 <= bytes) *reinterpret_cast<Vec *>(table + at) = Vec(0u);
+            else
+                for (int64_t b = at; b < bytes; b += 2) *reinterpret_cast<uint16_t *>(table + b) = 0;       // (elements of 2 or 4 bytes)
+        }
+        return;
+    }
+    __shared__ SortShared s;
+    const int64_t low = int64_t(blockIdx.x) * share, high = low + share < vocab ? low + share : vocab;
+    const int passes = bits <= kDigitBits ? 1 : (bits + kDigitBits - 1) / kDigitBits;
+    uint32_t ahead = 0, own = 0, base = 0, mine = 0;
+    bool counting = true;
+    const auto from_ids = [&](int64_t i, uint32_t &key, int32_t &token) {
+        const int64_t id = ids[i];
+        const bool valid = id >= 0 && id < vocab && id != ignore, in = valid && id >= low && id < high;
+        if (counting) {
+            ahead += valid && id < low;
+            own += in;
+        }
+        key = uint32_t(id - low);
+        token = int32_t(i);
+        return in;
+    };
+    const auto totals = [&] {
+        counting = false;
+        const uint32_t x = wave_sum(ahead), y = wave_sum(own);
+        if ((tid & 63) == 0) {
+            s.waves[tid >> 6] = x;
+            s.all[tid >> 6] = y;
+        }
+        __syncthreads();
+        for (int w = 0; w < kSortWaves; w++) {
+            base += s.waves[w];
+            mine += s.all[w];
+        }
+        if (blockIdx.x == sort_blocks - 1 && tid == 0) header->count = int32_t(base + mine);
+    };
+    int to = (passes - 1) & 1;
+    const auto put = [&](uint32_t place, uint32_t key, int32_t token) {
+        a.token[to][base + place] = token;
+        a.id[to][base + place] = int32_t(low + key);
+    };
+    const int first_bits = bits < kDigitBits ? bits : kDigitBits;
+    // (sort_pass has read s.waves before it calls this, but not all waves may be done with it)
+    sort_pass(s, tokens, 0, first_bits, from_ids, [&] { __syncthreads(); totals(); }, put);
+    for (int p = 1; p < passes; p++) {
+        const int from = to;
+        to ^= 1;
+        const int32_t *token = a.token[from] + base, *id = a.id[from] + base;
+        const auto from_list = [&](int64_t i, uint32_t &key, int32_t &t) {
+            key = uint32_t(id[i] - low);
+            t = token[i];
+            return true;
+        };
+        const int left = bits - p * kDigitBits;
+        sort_pass(s, int64_t(mine), p * kDigitBits, left < kDigitBits ? left : kDigitBits, from_list, [] {}, put);
+    }
+}
+
+// ---------------------------------------------------------------- gradient: sums
+
+template <typename T>
+__device__ __forceinline__ void finish(const float (&acc)[Piece<T>::V], float scale, bool accumulate, T *row, int64_t column, int64_t width)
+{
+    using P = Piece<T>;
+    typename P::Vec v;
+    if (accumulate) {
+        v = P::load(row, column, width);
+#pragma unroll
+        for (int e = 0; e < P::V; e++) v[e] = T(__builtin_fmaf(acc[e], scale, float(v[e])));
+    } else {
+#pragma unroll
+        for (int e = 0; e < P::V; e++) v[e] = T(acc[e] * scale);
+    }
+    P::store(row, column, width, v);
+}
+
+template <int V>
+__device__ __forceinline__ void put_partial(float *p, const float (&acc)[V])
+{
+    typedef float Four __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int e = 0; e < V; e += 4) *reinterpret_cast<Four *>(p + e) = Four{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+}
+
+// A wave sums one strip of a chunk of sorted tokens: kAhead rows are on their way at a time.  A run of tokens of one id that ends within the chunk
+// it began in is finished here; what a chunk has of a run that came from the chunk before, and of one that goes on in the next, is left for join_runs.
+constexpr int kAhead = 8;
+template <typename T>
+__global__ __launch_bounds__(kBlock) void sum_chunks(const EmbedHeader *header, const int32_t *__restrict__ tokens, const int32_t *__restrict__ ids,
+                                                     const T *__restrict__ dout, int64_t width, uint32_t strips, int32_t chunk, float scale,
+                                                     int32_t accumulate, T *__restrict__ dtable, float *__restrict__ partial, int64_t pitch)
+{
+    using P = Piece<T>;
+    const int lane = int(threadIdx.x) & 63;
+    const uint32_t item = blockIdx.x * (kBlock / 64) + uint32_t(__builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6));
+    const uint32_t at = item / strips, strip = item % strips;
+    const int64_t count = header->count, p0 = int64_t(at) * chunk;
+    if (p0 >= count) return;
+    const int n = int(count - p0 < chunk ? count - p0 : chunk);
+    const int32_t mine = lane < n ? ids[p0 + lane] : -1, from = lane < n ? tokens[p0 + lane] : 0;
+    const int32_t before = p0 > 0 ? ids[p0 - 1] : -1, after = p0 + n < count ? ids[p0 + n] : -1;
+    const int64_t column = (int64_t(strip) * 64 + lane) * P::V;
+    const bool there = column < width;
+    float acc[P::V];
+#pragma unroll
+    for (int e = 0; e < P::V; e++) acc[e] = 0.f;
+    int32_t id = __builtin_amdgcn_readlane(mine, 0);
+    bool carried = id == before;
+    for (int k0 = 0; k0 < n; k0 += kAhead) {
+        typename P::Vec v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            const int j = k0 + k < n ? k0 + k : n - 1;
+            const int64_t token = __builtin_amdgcn_readlane(from, j);
+            v[k] = there ? P::load(dout + token * width, column, width) : typename P::Vec(T(0.f));
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            if (k0 + k >= n) break;
+#pragma unroll
+            for (int e = 0; e < P::V; e++) acc[e] += float(v[k][e]);
+            const bool end = k0 + k + 1 == n;
+            const int32_t next = end ? after : __builtin_amdgcn_readlane(mine, (k0 + k + 1) & 63);
+            if (next == id && !end) continue;
+            const bool goes_on = next == id;
+            if (carried || goes_on) put_partial(partial + (int64_t(at) * 2 + (carried ? 0 : 1)) * pitch + column, acc);
+            else if (there) finish<T>(acc, scale, accumulate != 0, dtable + int64_t(id) * width, column, width);
+            carried = false;
+            id = next;
+#pragma unroll
+            for (int e = 0; e < P::V; e++) acc[e] = 0.f;
+        }
+    }
+}
+
+// Runs that go over the end of the chunk they began in: their parts, in order.  A block per chunk and strip, whose waves take a share of the
+// chunks each.
+constexpr int kJoinWaves = 8;
+template <typename T>
+__global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *header, const int32_t *__restrict__ ids, int64_t width,
+                                                             uint32_t strips, int32_t chunk, float scale, int32_t accumulate,
+                                                             T *__restrict__ dtable, const float *__restrict__ partial, int64_t pitch)
+{
+    using P = Piece<T>;
+    typedef float Four __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) float sums[kJoinWaves][64 * P::V];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int64_t at = blockIdx.x / strips, strip = blockIdx.x % strips;
+    const int64_t count = header->count, p0 = at * chunk;
+    if (p0 + chunk >= count) return;                     // nothing after this chunk
+    const int32_t id = ids[p0 + chunk - 1];
+    if (ids[p0 + chunk] != id || (p0 > 0 && ids[p0 - 1] == id)) return;
+    // the last chunk that begins with this id, 64 guesses at a time
+    int64_t last = at + 1, end = (count + chunk - 1) / chunk;
+    while (end - last > 1) {
+        const int64_t step = (end - last + 63) / 64, guess = last + lane * step;
+        const int same = __popcll(__ballot(guess < end && ids[(guess < end ? guess : last) * chunk] == id));
+        const int64_t found = last + int64_t(same - 1) * step;
+        end = found + step < end ? found + step : end;
+        last = found;
+    }
+    const int64_t column = (strip * 64 + lane) * P::V, parts = last - at, each = (parts + kJoinWaves - 1) / kJoinWaves;
+    const int64_t to = at + 1 + (wave + 1) * each < last + 1 ? at + 1 + (wave + 1) * each : last + 1;
+    float acc[P::V];
+    const auto add = [&](const float *p) {
+#pragma unroll
+        for (int e = 0; e < P::V; e += 4) {
+            const Four v = *reinterpret_cast<const Four *>(p + e);
+            acc[e] += v[0];
+            acc[e + 1] += v[1];
+            acc[e + 2] += v[2];
+            acc[e + 3] += v[3];
+        }
+    };
+#pragma unroll
+    for (int e = 0; e < P::V; e++) acc[e] = 0.f;
+    if (wave == 0) add(partial + (at * 2 + 1) * pitch + column);
+#pragma unroll 4
+    for (int64_t c = at + 1 + wave * each; c < to; c++) add(partial + c * 2 * pitch + column);
+    put_partial(&sums[wave][lane * P::V], acc);
+    __syncthreads();
+    if (wave != 0 || column >= width) return;
+#pragma unroll
+    for (int e = 0; e < P::V; e++) acc[e] = 0.f;
+    for (int w = 0; w < kJoinWaves; w++) add(&sums[w][lane * P::V]);
+    finish<T>(acc, scale, accumulate != 0, dtable + int64_t(id) * width, column, width);
+}
+
+// ---------------------------------------------------------------- launches
+
+struct Launches {
+    hipStream_t stream;
+    hipError_t error = hipSuccess;           // of the first launch that was refused
+    void launched()
+    {
+        const hipError_t e = hipGetLastError();
+        if (error == hipSuccess) error = e;
+    }
+};
+
+template <typename T>
+hipError_t look_up_all(const void *table, const int64_t *ids, int64_t tokens, int64_t width, int64_t vocab, int64_t ignore, float scale, void *out,
+                       hipStream_t stream)
+{
+    Launches l{stream};
+    const int64_t strips = (width + 64 * Piece<T>::V - 1) / (64 * Piece<T>::V);
+    const auto go = [&](auto each) {
+        constexpr int EACH = decltype(each)::value;
+        const int64_t parts = (strips + EACH - 1) / EACH;
+        look_up<T, EACH><<<dim3(uint32_t((tokens * parts + kBlock / 64 - 1) / (kBlock / 64))), kBlock, 0, stream>>>(
+            static_cast<const T *>(table), ids, tokens, width, vocab, ignore, scale, uint32_t(parts), static_cast<T *>(out));
+        l.launched();
+    };
+    if (strips >= 4 && tokens * strips >= 8192) go(std::integral_constant<int, 4>());
+    else if (strips >= 2 && tokens * strips >= 4096) go(std::integral_constant<int, 2>());
+    else go(std::integral_constant<int, 1>());
+    return l.error;
+}
+
+template <typename T>
+hipError_t gradient(const EmbedLayout &l, const void *dout, const int64_t *ids, int64_t ignore, float scale, bool accumulate, void *dtable,
+                    unsigned char *ws, hipStream_t stream)
+{
+    Launches g{stream};
+    const auto at = [ws](size_t offset) { return reinterpret_cast<int32_t *>(ws + offset); };
+    EmbedHeader *header = reinterpret_cast<EmbedHeader *>(ws);
+    const SortArrays a{{at(l.token[0]), at(l.token[1])}, {at(l.id[0]), at(l.id[1])}};
+    const int64_t bytes = l.vocab * l.width * int64_t(sizeof(T)), fills = accumulate ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
+    const uint32_t sorts = l.tokens ? uint32_t(l.blocks) : 0, grid = sorts + uint32_t(fills);
+    if (grid) {
+        if (fills)
+            sort_tokens<true><<<dim3(grid), kSortThreads, 0, stream>>>(ids, l.tokens, ignore, l.vocab, l.share, l.bits, sorts, header, a,
+                                                                       static_cast<unsigned char *>(dtable), bytes);
+        else
+            sort_tokens<false><<<dim3(grid), kSortThreads, 0, stream>>>(ids, l.tokens, ignore, l.vocab, l.share, l.bits, sorts, header, a, nullptr, 0);
+        g.launched();
+    }
+    if (!l.tokens) return g.error;
+    float *partial = reinterpret_cast<float *>(ws + l.partial);
+    const int64_t items = l.chunks * l.strips;
+    sum_chunks<T><<<dim3(uint32_t((items + kBlock / 64 - 1) / (kBlock / 64))), kBlock, 0, stream>>>(
+        header, a.token[0], a.id[0], static_cast<const T *>(dout), l.width, uint32_t(l.strips), l.chunk, scale, accumulate,
+        static_cast<T *>(dtable), partial, l.pitch);
+    g.launched();
+    if (l.chunks > 1) {
+        join_runs<T><<<dim3(uint32_t((l.chunks - 1) * l.strips)), 64 * kJoinWaves, 0, stream>>>(
+            header, a.id[0], l.width, uint32_t(l.strips), l.chunk, scale, accumulate, static_cast<T *>(dtable), partial, l.pitch);
+        g.launched();
+    }
+    return g.error;
+}
+
+}  // namespace
+
+int launch_embed(const void *table, const int64_t *ids, int64_t tokens, int64_t width, int64_t vocab, int dt, int64_t ignore, float scale,
+                 void *out, void *stream)
+{
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (dt == CGX_F32) return look_up_all<float>(table, ids, tokens, width, vocab, ignore, scale, out, s);
+    if (dt == CGX_F16) return look_up_all<_Float16>(table, ids, tokens, width, vocab, ignore, scale, out, s);
+    return look_up_all<__bf16>(table, ids, tokens, width, vocab, ignore, scale, out, s);
+}
+
+int launch_embed_grad(const EmbedLayout &l, const void *dout, const int64_t *ids, int64_t ignore, float scale, bool accumulate, void *dtable,
+                      unsigned char *workspace, void *stream)
+{
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (l.dt == CGX_F32) return gradient<float>(l, dout, ids, ignore, scale, accumulate, dtable, workspace, s);
+    if (l.dt == CGX_F16) return gradient<_Float16>(l, dout, ids, ignore, scale, accumulate, dtable, workspace, s);
+    return gradient<__bf16>(l, dout, ids, ignore, scale, accumulate, dtable, workspace, s);
+}
+
+}  // namespace cgx

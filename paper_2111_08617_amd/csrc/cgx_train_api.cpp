@@ -1,7 +1,8 @@
-// extern "C" entry points of what stands beside the fused buffer (see include/cgx.h): the head's loss and its gradient,
-// the gradients' norm and clipping.  Argument checks, then launches on the caller's stream.
+// extern "C" entry points of what stands beside the fused buffer (see include/cgx.h): the embedding and its gradient, the head's
+// losses and their gradients, the gradients' norm and clipping.  Argument checks, then launches on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include "cgx_embed.h"
 #include "cgx_grad.h"
 #include "cgx_head.h"
 
@@ -72,6 +73,40 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
     if (workspace_bytes < l.bytes) return CGX_ERR_SIZE;
     return status_of(cgx::launch_head_loss_grad(l, {hidden, weight, targets, ignore, static_cast<unsigned char *>(workspace)}, lse, dloss,
                                                 dhidden, dweight, stream));
+}
+
+int cgx_embed(const void *table, const int64_t *ids, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, int64_t ignore, float scale,
+              void *out, void *stream)
+{
+    cgx::EmbedLayout l;
+    const int rc = cgx::embed_layout(tokens, width, vocab, int(dt), &l);
+    if (rc != CGX_OK) return rc;
+    if (tokens == 0) return CGX_OK;
+    if (!table || !ids || !out) return CGX_ERR_NULL;
+    if (misaligned(table) || misaligned(ids, 8) || misaligned(out)) return CGX_ERR_ALIGN;
+    return status_of(cgx::launch_embed(table, ids, tokens, width, vocab, int(dt), ignore, scale, out, stream));
+}
+
+int cgx_embed_grad_workspace(int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, size_t *bytes)
+{
+    cgx::EmbedLayout l;
+    const int rc = cgx::embed_layout(tokens, width, vocab, int(dt), &l);
+    if (rc != CGX_OK) return rc;
+    if (!bytes) return CGX_ERR_NULL;
+    *bytes = l.bytes;
+    return CGX_OK;
+}
+
+int cgx_embed_grad(const void *dout, const int64_t *ids, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, int64_t ignore, float scale,
+                   int32_t accumulate, void *dtable, void *workspace, size_t workspace_bytes, void *stream)
+{
+    cgx::EmbedLayout l;
+    const int rc = cgx::embed_layout(tokens, width, vocab, int(dt), &l);
+    if (rc != CGX_OK) return rc;
+    if (!dtable || !workspace || (tokens > 0 && (!dout || !ids))) return CGX_ERR_NULL;
+    if (misaligned(dout) || misaligned(ids, 8) || misaligned(dtable) || misaligned(workspace)) return CGX_ERR_ALIGN;
+    if (workspace_bytes < l.bytes) return CGX_ERR_SIZE;
+    return status_of(cgx::launch_embed_grad(l, dout, ids, ignore, scale, accumulate != 0, dtable, static_cast<unsigned char *>(workspace), stream));
 }
 
 int cgx_grad_norm_workspace(size_t *bytes)
