@@ -438,6 +438,36 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
                        void *stream);
 
 /*
+ * Distillation through the head: the Kullback-Leibler divergence of the student's softmax, over its whole vocabulary, from a teacher's, over the
+ * few largest logits that are kept of it; without the student's logits.  z as above, T the temperature:
+ *   q[n][k]   = softmax over token n's entries of teacher[n][k] / T
+ *   lse[n]    = log(sum_v exp(z[n][v] / T)),  picked[n][k] = z[n][ids[n][k]]
+ *   loss[n]   = sum_k q[n][k] (log q[n][k] + lse[n] - picked[n][k] / T)
+ * cgx_head_distill writes loss, lse and picked.  Given that lse and picked and one factor per token (dloss, with the T^2 that some put in front
+ * of the loss, and the share of this loss in the step's), cgx_head_distill_grad writes
+ *   d[n][v]   = dloss[n] / T (exp(z[n][v] / T - lse[n]) - sum_{k: ids[n][k] = v} q[n][k])
+ * and dhidden, dweight as above.  Everything that is said above of logits, d, sums, hidden, weight, loss, lse, dloss, dhidden, dweight, overlaps
+ * and sizes holds here too, with these arguments instead of targets:
+ *   ids       device, tokens x entries int64 (8-byte aligned), in any order.  An entry that is `ignore` is none: its logit is not looked at and its
+ *             picked is 0.  Entries of one token with the same id count as their sum.  Any other id outside [0, vocab) makes that token's
+ *             loss and gradients NaN, and its picked.
+ *   teacher   device, tokens x entries elements of teacher_dt (CGX_F32, CGX_F16 or CGX_BF16), aligned like its elements.  -infinity is a share of 0;
+ *             NaN and +infinity make that token's loss and gradients NaN.
+ *   picked    device, tokens x entries floats (4-byte aligned)
+ * A token without an entry, or whose entries all have a share of 0, takes no part: loss, lse and picked 0, a dhidden row of zeros, nothing in
+ * dweight, whatever its hidden state holds; so does, in cgx_head_distill_grad, one whose dloss is 0.
+ * 1 <= entries <= 1024 (more than vocab are allowed), 2^-64 <= temperature <= 2^64 (CGX_ERR_SIZE otherwise).
+ */
+int cgx_head_distill_workspace(int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt,
+                               int32_t grad /* 0: for cgx_head_distill; else for both calls */, size_t *bytes);
+int cgx_head_distill(const void *hidden, const void *weight, const int64_t *ids, const void *teacher, int64_t tokens, int32_t width, int64_t vocab,
+                     int32_t entries, cgx_dtype dt, cgx_dtype teacher_dt, int64_t ignore, float temperature, float *loss, float *lse, float *picked,
+                     void *workspace, size_t workspace_bytes, void *stream);
+int cgx_head_distill_grad(const void *hidden, const void *weight, const int64_t *ids, const void *teacher, const float *lse, const float *picked,
+                          const float *dloss, int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt, cgx_dtype teacher_dt,
+                          int64_t ignore, float temperature, void *dhidden, void *dweight, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Embedding: rows of a table for a list of tokens, and the table's gradient.
  *   cgx_embed       out[n][h] = scale * table[ids[n]][h]
  *   cgx_embed_grad  dtable[v][h] = scale * sum_{n: ids[n] = v} dout[n][h]  (+ dtable[v][h] with accumulate)

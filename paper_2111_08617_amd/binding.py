@@ -33,7 +33,7 @@ EXPORTS = ("cgx_sizes", "cgx_quantize", "cgx_dequant_reduce", "cgx_dequant_reduc
            "cgx_qsgd_layered_quantize", "cgx_qsgd_layered_dequant_reduce", "cgx_qsgd_layered_dequant_reduce_requantize",
            "cgx_plan_tiles", "cgx_plan_tiles_chunk", "cgx_stream_probe", "cgx_stream_probe_shaped",
            "cgx_issue_probe", "cgx_issue_probe_form", "cgx_head_workspace", "cgx_head_loss", "cgx_head_loss_grad",
-           "cgx_embed", "cgx_embed_grad_workspace", "cgx_embed_grad",
+           "cgx_head_distill_workspace", "cgx_head_distill", "cgx_head_distill_grad", "cgx_embed", "cgx_embed_grad_workspace", "cgx_embed_grad",
            "cgx_grad_norm_workspace", "cgx_grad_norm", "cgx_grad_clip", "cgx_status_string", "cgx_shutdown")
 
 TILE_DTYPE = np.dtype([("elem0", "<i8"), ("packed_off", "<i8"), ("bucket0", "<u4"), ("count", "<u4"),
@@ -117,6 +117,10 @@ def lib() -> ctypes.CDLL:
                                     c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
         L.cgx_head_loss_grad.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64,
                                          c.c_int, c.c_int64, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.cgx_head_distill_workspace.argtypes = [c.c_int64, c.c_int32, c.c_int64, c.c_int32, c.c_int, c.c_int32, c.POINTER(c.c_size_t)]
+        sizes = [c.c_int64, c.c_int32, c.c_int64, c.c_int32, c.c_int, c.c_int, c.c_int64, c.c_float]
+        L.cgx_head_distill.argtypes = [c.c_void_p] * 4 + sizes + [c.c_void_p] * 4 + [c.c_size_t, c.c_void_p]
+        L.cgx_head_distill_grad.argtypes = [c.c_void_p] * 7 + sizes + [c.c_void_p] * 3 + [c.c_size_t, c.c_void_p]
         L.cgx_embed.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int64, c.c_float, c.c_void_p, c.c_void_p]
         L.cgx_embed_grad_workspace.argtypes = [c.c_int64, c.c_int32, c.c_int64, c.c_int, c.POINTER(c.c_size_t)]
         L.cgx_embed_grad.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int, c.c_int64, c.c_float, c.c_int32,
@@ -713,6 +717,73 @@ def _here(name: str, stream, *tensors) -> int:
         if t.get_device() != device:
             raise ValueError(f"{name}: {what}: the tensor lives on {t.device}, the call runs on the current device, cuda:{device}")
     return _stream(stream)
+
+
+def cgx_head_distill_workspace(tokens: int, width: int, vocab: int, entries: int, dt: int, grad: bool = False) -> int:
+    """Bytes of device workspace cgx_head_distill needs; with grad, cgx_head_distill_grad as well."""
+    nbytes = ctypes.c_size_t()
+    _check(lib().cgx_head_distill_workspace(_held(tokens, 64), _held(width, 32), _held(vocab, 64), _held(entries, 32), _held(dt, 32),
+                                            int(bool(grad)), ctypes.byref(nbytes)), "cgx_head_distill_workspace")
+    return int(nbytes.value)
+
+
+def _distill(name: str, hidden, weight, ids, teacher, ignore: int, temperature: float):
+    """(addresses of hidden, weight, ids and teacher; the sizes, types, mark and temperature behind them; tokens, width, vocab, entries, dt)."""
+    for t, what, rows in ((hidden, "hidden", "token"), (weight, "weight", "entry of the vocabulary"), (ids, "ids", "token"), (teacher, "teacher", "token")):
+        if getattr(t, "ndim", 0) != 2:
+            raise ValueError(f"{name}: {what}: a matrix is needed, a row for each {rows}")
+    (tokens, width), (vocab, across), (rows, entries) = hidden.shape, weight.shape, ids.shape
+    dt, teacher_dt = _HEAD_TYPES.get(str(hidden.dtype)), _HEAD_TYPES.get(str(teacher.dtype))
+    for t, what, known in ((hidden, "hidden", dt), (teacher, "teacher", teacher_dt)):
+        if known is None:
+            raise ValueError(f"{name}: {what}: element type {t.dtype}, expected torch.float32, torch.float16 or torch.bfloat16")
+    if across != width:
+        raise ValueError(f"{name}: weight: rows of {across} elements, those of hidden have {width}")
+    if rows != tokens:
+        raise ValueError(f"{name}: ids: {rows} rows for {tokens} tokens")
+    if tuple(teacher.shape) != (rows, entries):
+        raise ValueError(f"{name}: teacher: {tuple(teacher.shape)} logits for {(rows, entries)} ids")
+    size = 4 if dt == F32 else 2
+    return ((_device_buffer(hidden, (name, "hidden"), tokens * width * size, _TORCH_NAMES[dt]),
+             _device_buffer(weight, (name, "weight"), vocab * width * size, _TORCH_NAMES[dt]),
+             _device_buffer(ids, (name, "ids"), tokens * entries * 8, "int64"),
+             _device_buffer(teacher, (name, "teacher"), tokens * entries * (4 if teacher_dt == F32 else 2), _TORCH_NAMES[teacher_dt])),
+            (tokens, _held(width, 32), vocab, _held(entries, 32), dt, teacher_dt, _mark(name, ignore), float(temperature)),
+            (tokens, width, vocab, entries, dt))
+
+
+def cgx_head_distill(hidden, weight, ids, teacher, loss, lse, picked, workspace, temperature: float = 1.0, ignore: int = -100, stream=None) -> None:
+    """Divergence of the softmax of (hidden @ weight.T) / temperature from a teacher's, given by its largest logits, without the student's:
+    loss and lse (device float32[tokens]) of every token, and picked (float32[tokens, entries]), the student's logits at the teacher's entries.
+    ids (int64) and teacher (float32, float16 or bfloat16): [tokens, entries]; `ignore` marks entries that are none; workspace: device
+    tensor of cgx_head_distill_workspace bytes.  The other arguments are those of cgx_head_loss."""
+    name = "cgx_head_distill"
+    addresses, arguments, (tokens, _, _, entries, _) = _distill(name, hidden, weight, ids, teacher, ignore, temperature)
+    out, sums = (_device_buffer(x, (name, what), tokens * 4, "float32") for x, what in ((loss, "loss"), (lse, "lse")))
+    at = _device_buffer(picked, (name, "picked"), tokens * entries * 4, "float32")
+    ws = _device_buffer(workspace, (name, "workspace"), 0)
+    where = _here(name, stream, (hidden, "hidden"), (weight, "weight"), (ids, "ids"), (teacher, "teacher"), (loss, "loss"), (lse, "lse"),
+                  (picked, "picked"), (workspace, "workspace"))
+    _check(lib().cgx_head_distill(*addresses, *arguments, out, sums, at, ws, workspace.numel() * workspace.element_size(), where), name)
+
+
+def cgx_head_distill_grad(hidden, weight, ids, teacher, lse, picked, dloss, dhidden, dweight, workspace, temperature: float = 1.0, ignore: int = -100,
+                          stream=None) -> None:
+    """Gradients of sum(dloss * loss) by hidden and weight, into dhidden and dweight (their shapes and type).  lse and picked: from
+    cgx_head_distill of the same arguments; dloss: device float32[tokens], 0 for tokens that take no part; workspace: device tensor of
+    cgx_head_distill_workspace(..., grad=True) bytes."""
+    name = "cgx_head_distill_grad"
+    addresses, arguments, (tokens, width, vocab, entries, dt) = _distill(name, hidden, weight, ids, teacher, ignore, temperature)
+    size = 4 if dt == F32 else 2
+    sums, factors = (_device_buffer(x, (name, what), tokens * 4, "float32") for x, what in ((lse, "lse"), (dloss, "dloss")))
+    at = _device_buffer(picked, (name, "picked"), tokens * entries * 4, "float32")
+    dh = _device_buffer(dhidden, (name, "dhidden"), tokens * width * size, _TORCH_NAMES[dt])
+    dw = _device_buffer(dweight, (name, "dweight"), vocab * width * size, _TORCH_NAMES[dt])
+    ws = _device_buffer(workspace, (name, "workspace"), 0)
+    where = _here(name, stream, (hidden, "hidden"), (weight, "weight"), (ids, "ids"), (teacher, "teacher"), (lse, "lse"), (picked, "picked"),
+                  (dloss, "dloss"), (dhidden, "dhidden"), (dweight, "dweight"), (workspace, "workspace"))
+    _check(lib().cgx_head_distill_grad(*addresses[:4], sums, at, factors, *arguments, dh, dw, ws, workspace.numel() * workspace.element_size(),
+                                       where), name)
 
 
 def _embedding(name: str, table, what: str, ids, rows, across: str):

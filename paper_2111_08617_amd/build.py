@@ -21,6 +21,7 @@ SOURCES = [("cgx_plan.cpp", "cgx_plan", []), ("cgx_api.cpp", "cgx_api", []), ("c
            ("cgx_stats.hip", "cgx_stats", []),
            ("cgx_probe.hip", "cgx_probe", []), ("cgx_train_api.cpp", "cgx_train_api", []), ("cgx_head.cpp", "cgx_head_layout", []),
            ("cgx_head.hip", "cgx_head", []), ("cgx_grad.hip", "cgx_grad", []),
+           ("cgx_distill.cpp", "cgx_distill_layout", []), ("cgx_distill.hip", "cgx_distill", []),
            ("cgx_embed.cpp", "cgx_embed_layout", []), ("cgx_embed.hip", "cgx_embed", [])]
 
 # -ffp-contract=off: the code decision is binary32 without fused operations.

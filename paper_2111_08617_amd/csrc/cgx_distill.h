@@ -1,0 +1,36 @@
+// The head's calls that learn from a teacher's entries (include/cgx.h, cgx_head_distill*): sizes and workspace layout, and
+// launchers (cgx_distill.hip).
+#pragma once
+
+#include "cgx_head.h"
+
+namespace cgx {
+
+constexpr int kMostEntries = 1024;                   // of the teacher, a token
+
+struct DistillLayout {
+    HeadLayout head;
+    int32_t entries = 0;
+    size_t mark = 0;         // int64 [tokens]: what the head's list reads as targets: kTakesPart, kNoPart or (kWrong) not a number
+    size_t bytes = 0;
+};
+
+// CGX_OK and the layout, or the error of the sizes.
+int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries, int dt, bool grad, DistillLayout *out);
+
+// Device addresses of a call, and its temperature.
+struct DistillBuffers {
+    const void *hidden, *weight;
+    const int64_t *ids;
+    const void *teacher;
+    int teacher_dt;
+    int64_t ignore;
+    float temperature;
+    unsigned char *workspace;
+};
+// The stream is a hipStream_t; the result a hipError_t.
+int launch_distill(const DistillLayout &l, const DistillBuffers &b, float *loss, float *lse, float *picked, void *stream);
+int launch_distill_grad(const DistillLayout &l, const DistillBuffers &b, const float *lse, const float *picked, const float *dloss,
+                        void *dhidden, void *dweight, void *stream);
+
+}  // namespace cgx

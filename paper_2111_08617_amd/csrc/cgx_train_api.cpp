@@ -2,6 +2,7 @@
 // losses and their gradients, the gradients' norm and clipping.  Argument checks, then launches on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include "cgx_distill.h"
 #include "cgx_embed.h"
 #include "cgx_grad.h"
 #include "cgx_head.h"
@@ -27,6 +28,16 @@ int check_tensors(const cgx_tensor *tensors, int32_t count)
         if (t.n > 0 && misaligned(t.data, t.dt == CGX_F32 ? 4 : 2)) return CGX_ERR_ALIGN;
     }
     return CGX_OK;
+}
+
+// Sizes, types and temperature of a call that learns from a teacher's entries.
+int check_distill(int64_t tokens, int32_t width, int64_t vocab, int32_t entries, int dt, int teacher_dt, float temperature, bool grad,
+                  cgx::DistillLayout *l)
+{
+    const int rc = cgx::distill_layout(tokens, width, vocab, entries, dt, grad, l);
+    if (rc != CGX_OK) return rc;
+    if (!known_type(teacher_dt)) return CGX_ERR_DTYPE;
+    return temperature >= 0x1p-64f && temperature <= 0x1p64f ? CGX_OK : CGX_ERR_SIZE;
 }
 
 }  // namespace
@@ -73,6 +84,50 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
     if (workspace_bytes < l.bytes) return CGX_ERR_SIZE;
     return status_of(cgx::launch_head_loss_grad(l, {hidden, weight, targets, ignore, static_cast<unsigned char *>(workspace)}, lse, dloss,
                                                 dhidden, dweight, stream));
+}
+
+int cgx_head_distill_workspace(int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt, int32_t grad, size_t *bytes)
+{
+    cgx::DistillLayout l;
+    const int rc = cgx::distill_layout(tokens, width, vocab, entries, int(dt), grad != 0, &l);
+    if (rc != CGX_OK) return rc;
+    if (!bytes) return CGX_ERR_NULL;
+    *bytes = l.bytes;
+    return CGX_OK;
+}
+
+int cgx_head_distill(const void *hidden, const void *weight, const int64_t *ids, const void *teacher, int64_t tokens, int32_t width, int64_t vocab,
+                     int32_t entries, cgx_dtype dt, cgx_dtype teacher_dt, int64_t ignore, float temperature, float *loss, float *lse, float *picked,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    cgx::DistillLayout l;
+    const int rc = check_distill(tokens, width, vocab, entries, int(dt), int(teacher_dt), temperature, false, &l);
+    if (rc != CGX_OK) return rc;
+    if (tokens == 0) return CGX_OK;
+    if (!hidden || !weight || !ids || !teacher || !loss || !lse || !picked || !workspace) return CGX_ERR_NULL;
+    if (misaligned(hidden) || misaligned(weight) || misaligned(workspace) || misaligned(ids, 8) || misaligned(teacher, teacher_dt == CGX_F32 ? 4 : 2) ||
+        misaligned(loss, 4) || misaligned(lse, 4) || misaligned(picked, 4))
+        return CGX_ERR_ALIGN;
+    if (workspace_bytes < l.bytes) return CGX_ERR_SIZE;
+    return status_of(cgx::launch_distill(l, {hidden, weight, ids, teacher, int(teacher_dt), ignore, temperature, static_cast<unsigned char *>(workspace)},
+                                         loss, lse, picked, stream));
+}
+
+int cgx_head_distill_grad(const void *hidden, const void *weight, const int64_t *ids, const void *teacher, const float *lse, const float *picked,
+                          const float *dloss, int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt, cgx_dtype teacher_dt,
+                          int64_t ignore, float temperature, void *dhidden, void *dweight, void *workspace, size_t workspace_bytes, void *stream)
+{
+    cgx::DistillLayout l;
+    const int rc = check_distill(tokens, width, vocab, entries, int(dt), int(teacher_dt), temperature, true, &l);
+    if (rc != CGX_OK) return rc;
+    if (!weight || !dweight || !workspace) return CGX_ERR_NULL;
+    if (tokens > 0 && (!hidden || !ids || !teacher || !lse || !picked || !dloss || !dhidden)) return CGX_ERR_NULL;
+    if (misaligned(hidden) || misaligned(weight) || misaligned(workspace) || misaligned(dhidden) || misaligned(dweight) || misaligned(ids, 8) ||
+        misaligned(teacher, teacher_dt == CGX_F32 ? 4 : 2) || misaligned(lse, 4) || misaligned(picked, 4) || misaligned(dloss, 4))
+        return CGX_ERR_ALIGN;
+    if (workspace_bytes < l.bytes) return CGX_ERR_SIZE;
+    return status_of(cgx::launch_distill_grad(l, {hidden, weight, ids, teacher, int(teacher_dt), ignore, temperature, static_cast<unsigned char *>(workspace)},
+                                              lse, picked, dloss, dhidden, dweight, stream));
 }
 
 int cgx_embed(const void *table, const int64_t *ids, int64_t tokens, int32_t width, int64_t vocab, cgx_dtype dt, int64_t ignore, float scale,
