@@ -456,7 +456,7 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  *   picked    device, tokens x entries floats (4-byte aligned)
  * A token without an entry, or whose entries all have a share of 0, takes no part: loss, lse and picked 0, a dhidden row of zeros, nothing in
  * dweight, whatever its hidden state holds; so does, in cgx_head_distill_grad, one whose dloss is 0.
- * 1 <= entries <= 1024 (more than vocab are allowed), 2^-64 <= temperature <= 2^64 (CGX_ERR_SIZE otherwise).
+ * 1 <= entries <= 1024 (more than vocab are allowed), tokens x entries < 2^31, 2^-64 <= temperature <= 2^64 (CGX_ERR_SIZE otherwise).
  */
 int cgx_head_distill_workspace(int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt,
                                int32_t grad /* 0: for cgx_head_distill; else for both calls */, size_t *bytes);

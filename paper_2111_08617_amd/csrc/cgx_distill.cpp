@@ -8,10 +8,33 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     DistillLayout l;
     const int rc = head_layout(tokens, width, vocab, dt, grad, &l.head);
     if (rc != CGX_OK) return rc;
-    if (entries < 1 || entries > kMostEntries) return CGX_ERR_SIZE;
+    if (entries < 1 || entries > kMostEntries || tokens * entries >= int64_t(1) << 31) return CGX_ERR_SIZE;
     l.entries = entries;
-    l.mark = l.head.bytes;
-    l.bytes = l.mark + size_t((tokens * 8 + 255) / 256 * 256);
+    // (with more entries than this in every 64 columns a tile's end would take longer than the tile)
+    l.tiles = int64_t(entries) * 64 <= 4 * vocab;
+    l.strips = (vocab + 127) / 128 * 2;
+    size_t at = l.head.bytes;
+    const auto take = [&at](int64_t bytes) {
+        const size_t here = at;
+        at += size_t((bytes + 255) / 256 * 256);
+        return here;
+    };
+    l.mark = take(tokens * 8);
+    l.token = take(tokens * 4);
+    l.entry = take(tokens * entries * 8);
+    // the shares are the gradient call's, the strips the loss's
+    const size_t shared = at;
+    size_t end = at;
+    if (l.tiles) {
+        l.strip = take(tokens * l.strips * 2);
+        end = at;
+    }
+    if (grad) {
+        at = shared;
+        l.share = take(tokens * entries * 4);
+        end = at > end ? at : end;
+    }
+    l.bytes = end;
     *out = l;
     return CGX_OK;
 }

@@ -11,7 +11,13 @@ constexpr int kMostEntries = 1024;                   // of the teacher, a token
 struct DistillLayout {
     HeadLayout head;
     int32_t entries = 0;
+    bool tiles = false;      // the loss picks the student's logits out of the tiles they are formed in
+    int64_t strips = 0;      // of 64 columns of the vocabulary, rounded up to an even number
     size_t mark = 0;         // int64 [tokens]: what the head's list reads as targets: kTakesPart, kNoPart or (kWrong) not a number
+    size_t token = 0;        // int32 [tokens]: of a row of the list
+    size_t entry = 0;        // Entry [tokens][entries]: sorted by id; those that are none are the last, with an id of -1
+    size_t share = 0;        // float [tokens][entries] (gradient): of the entries in that order; ids that come again have theirs added to the first
+    size_t strip = 0;        // uint16 [tokens][strips] (loss, tiles): see Picks
     size_t bytes = 0;
 };
 

@@ -59,14 +59,95 @@ __device__ __forceinline__ TeacherRow teacher_row(const Teacher &t, int64_t toke
     return r;
 }
 
-// Which tokens take part: a wave per token.
-__global__ __launch_bounds__(256) void mark_tokens(Teacher teacher, int64_t tokens, int64_t *__restrict__ mark)
+// What the kernels after it need of a teacher's rows, a wave per token: which tokens take part; their entries sorted by id; and, for the loss, where
+// those of every 64 columns begin, for the gradient, their shares.  M: entries, rounded up to a power of two.
+constexpr int kRowWaves = 4;
+template <int M>
+struct RowShared {
+    uint64_t key[M];         // id, then place
+    float share[M];
+};
+
+// In ascending order, by one wave.  (LDS accesses of a wave are in order; the compiler is told not to move them.)
+__device__ __forceinline__ void wave_fence()
 {
-    const int lane = int(threadIdx.x) & 63;
-    const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (token >= tokens) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+template <int M>
+__device__ __forceinline__ void sort_keys(uint64_t *key, int lane)
+{
+    for (int run = 2; run <= M; run *= 2)
+        for (int apart = run / 2; apart > 0; apart /= 2) {
+            wave_fence();
+            for (int p = lane; p < M / 2; p += 64) {
+                const int low = 2 * apart * (p / apart) + p % apart, high = low + apart;
+                const uint64_t a = key[low], b = key[high];
+                const bool rising = (low & run) == 0;
+                if ((a > b) == rising) {
+                    key[low] = b;
+                    key[high] = a;
+                }
+            }
+        }
+    wave_fence();
+}
+
+template <int M, bool GRAD>
+__global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, int64_t tokens, int64_t *__restrict__ mark,
+                                                               Entry *__restrict__ entries, float *__restrict__ shares,
+                                                               uint16_t *__restrict__ strips, int64_t pitch)
+{
+    __shared__ RowShared<M> all[kRowWaves];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int64_t token = int64_t(blockIdx.x) * kRowWaves + wave;
+    if (token >= tokens) return;                         // (no barriers of blocks follow)
+    RowShared<M> &s = all[wave];
     const TeacherRow r = teacher_row(teacher, token, lane);
     if (lane == 0) mark[token] = r.wrong ? kWrong : r.takes_part() ? kTakesPart : kNoPart;
+    if (!r.takes_part()) return;
+    const int64_t first = token * teacher.entries;
+    constexpr uint64_t kNone = ~uint64_t(0);
+    for (int k = lane; k < M; k += 64) {
+        uint64_t key = kNone;
+        if (k < teacher.entries) {
+            const int64_t id = teacher.ids[first + k];
+            if (id != teacher.ignore && id >= 0 && id < teacher.vocab) key = uint64_t(id) << kStripBits | uint64_t(k);
+            if (GRAD) s.share[k] = key == kNone ? 0.f : r.share(teacher.logit(first + k) * teacher.inverse);
+        }
+        s.key[k] = key;
+    }
+    sort_keys<M>(s.key, lane);
+    const auto id_of = [](uint64_t key) { return int32_t(key >> kStripBits); };
+    for (int k = lane; k < teacher.entries; k += 64) {
+        const uint64_t key = s.key[k];
+        const int32_t place = int32_t(key & ((1u << kStripBits) - 1));
+        Entry e{key == kNone ? -1 : id_of(key), place};
+        if (GRAD && e.id >= 0) {
+            if (k > 0 && id_of(s.key[k - 1]) == e.id) e.id = -1;
+            else {
+                float q = s.share[place];
+                for (int j = k + 1; j < teacher.entries && s.key[j] != kNone && id_of(s.key[j]) == e.id; j++)
+                    q += s.share[int32_t(s.key[j] & ((1u << kStripBits) - 1))];
+                shares[first + k] = q;
+            }
+        }
+        entries[first + k] = e;
+    }
+    if (GRAD || !strips) return;
+    // (entries that are none come after all strips)
+    const auto begin = [&](int64_t id) {
+        int low = 0;
+#pragma unroll
+        for (int step = M / 2; step > 0; step /= 2)
+            if (s.key[low + step - 1] < uint64_t(id) << kStripBits) low += step;
+        return low + (s.key[low] < uint64_t(id) << kStripBits ? 1 : 0);
+    };
+    const int64_t used = (teacher.vocab + kStripColumns - 1) / kStripColumns;
+    for (int64_t strip = lane; strip < used; strip += 64) {
+        const int from = begin(strip * kStripColumns), to = begin((strip + 1) * kStripColumns), n = to - from;
+        strips[token * pitch + strip] = n ? uint16_t(uint32_t(from) | uint32_t(n < int(kStripMost) ? n : int(kStripMost)) << kStripBits) : uint16_t(0);
+    }
 }
 
 // 16 bytes of a row that starts at any element, as binary32.
@@ -88,6 +169,36 @@ struct Slice {
         }
     }
 };
+
+// The loss from the tiles' parts of a token's softmax and its picked logits: a wave per token.
+__global__ __launch_bounds__(256) void join_picked(Teacher teacher, int64_t tokens, const int32_t *__restrict__ place, int64_t parts, int64_t pitch,
+                                                   const float2 *__restrict__ stats, float *__restrict__ loss, float *__restrict__ lse,
+                                                   float *__restrict__ picked)
+{
+    const int lane = int(threadIdx.x) & 63;
+    const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (token >= tokens) return;
+    const TeacherRow row = teacher_row(teacher, token, lane);
+    const int64_t first = token * teacher.entries;
+    const bool takes_part = row.takes_part();
+    const float total = takes_part ? log_sum<1>(stats + int64_t(place[token]) * pitch, parts, lane) : 0.f;
+    const float log_mass = row.top + logf(row.sum);
+    float sum = 0.f;
+    for (int k = lane; k < teacher.entries; k += 64) {
+        const int64_t id = teacher.ids[first + k];
+        if (!takes_part || id == teacher.ignore) picked[first + k] = 0.f;
+        else if (id < 0 || id >= teacher.vocab) picked[first + k] = __builtin_nanf("");
+        else {
+            const float scaled = teacher.logit(first + k) * teacher.inverse, q = row.share(scaled);
+            if (q > 0.f) sum += q * (scaled - log_mass + total - picked[first + k] * teacher.inverse);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if (lane != 0) return;
+    lse[token] = total;
+    loss[token] = !takes_part ? 0.f : row.wrong ? __builtin_nanf("") : sum;
+}
 
 // Joins the parts of a token's softmax, takes the student's logits at the teacher's entries (a wave per entry, four at a time), and the divergence.
 // A block of WAVES waves per token.
@@ -153,45 +264,23 @@ __global__ __launch_bounds__(64 * WAVES) void join_divergence(Teacher teacher, c
     loss[token] = row.wrong ? __builtin_nanf("") : sum;
 }
 
-// d at the teacher's entries within a piece of the vocabulary, in its units: a wave per token.  An id that comes several times in a row has the sum of
-// its shares, written by the first of them.
-constexpr int kEntryWaves = 4;
+// d at the teacher's entries within a piece of the vocabulary, in its units: a thread per entry.
 template <typename T>
-__global__ __launch_bounds__(64 * kEntryWaves) void delta_entries(Teacher teacher, const int32_t *__restrict__ place, int64_t tokens,
-                                                                  const float *__restrict__ lse, const float *__restrict__ factor,
-                                                                  const float *__restrict__ picked, int64_t from, int64_t columns,
-                                                                  T *__restrict__ delta, int64_t piece)
+__global__ __launch_bounds__(256) void delta_entries(const Entry *__restrict__ entries, const float *__restrict__ shares, int32_t count, int64_t all,
+                                                     const int32_t *__restrict__ place, const float *__restrict__ lse,
+                                                     const float *__restrict__ factor, const float *__restrict__ picked, float inverse, int64_t from,
+                                                     int64_t columns, T *__restrict__ delta, int64_t piece)
 {
-    __shared__ int32_t ids[kEntryWaves][kMostEntries];
-    __shared__ float shares[kEntryWaves][kMostEntries];
-    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int64_t token = int64_t(blockIdx.x) * kEntryWaves + wave;
-    const int32_t row = token < tokens ? place[token] : -1;
-    const int64_t first = token * teacher.entries;
-    if (row >= 0) {
-        const TeacherRow r = teacher_row(teacher, token, lane);
-        for (int k = lane; k < teacher.entries; k += 64) {
-            const int64_t id = teacher.ids[first + k];
-            const bool inside = id != teacher.ignore && id >= 0 && id < teacher.vocab;
-            ids[wave][k] = inside ? int32_t(id) : -1;
-            shares[wave][k] = inside ? r.share(teacher.logit(first + k) * teacher.inverse) : 0.f;
-        }
-    }
-    __syncthreads();
-    if (row < 0) return;
-    const float base = lse[row], f = factor[row];
-    for (int k = lane; k < teacher.entries; k += 64) {
-        const int64_t column = int64_t(ids[wave][k]) - from;
-        if (column < 0 || column >= columns || ids[wave][k] < 0) continue;
-        float q = 0.f;
-        bool again = false;
-        for (int j = 0; j < teacher.entries; j++) {
-            if (ids[wave][j] != ids[wave][k]) continue;
-            q += shares[wave][j];
-            again |= j < k;
-        }
-        if (!again) delta[row * piece + column] = T((lifted<T>(picked[first + k] * teacher.inverse, base) - q * float(1 << lift_of<T>)) * f);
-    }
+    const int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (k >= all) return;
+    const int64_t token = k / count;
+    const int32_t row = place[token];
+    if (row < 0) return;                                 // (it may have no sorted entries)
+    const Entry e = entries[k];
+    const int64_t column = e.id - from;
+    if (e.id < 0 || column < 0 || column >= columns) return;
+    const float z = picked[token * count + e.place];
+    delta[row * piece + column] = T((lifted<T>(z * inverse, lse[row]) - shares[k] * float(1 << lift_of<T>)) * factor[row]);
 }
 
 Teacher teacher_of(const DistillLayout &l, const DistillBuffers &b)
@@ -199,10 +288,19 @@ Teacher teacher_of(const DistillLayout &l, const DistillBuffers &b)
     return Teacher{b.ids, b.teacher, l.entries, b.teacher_dt, b.ignore, l.head.vocab, 1.f / b.temperature};
 }
 
-hipError_t mark(const DistillLayout &l, const DistillBuffers &b, hipStream_t stream)
+template <bool GRAD>
+hipError_t rows(const DistillLayout &l, const DistillBuffers &b, hipStream_t stream)
 {
-    mark_tokens<<<dim3(uint32_t((l.head.tokens + 3) / 4)), 256, 0, stream>>>(teacher_of(l, b), l.head.tokens,
-                                                                             reinterpret_cast<int64_t *>(b.workspace + l.mark));
+    const auto go = [&](auto most) {
+        constexpr int M = decltype(most)::value;
+        teacher_rows<M, GRAD><<<dim3(uint32_t((l.head.tokens + kRowWaves - 1) / kRowWaves)), 64 * kRowWaves, 0, stream>>>(
+            teacher_of(l, b), l.head.tokens, reinterpret_cast<int64_t *>(b.workspace + l.mark), reinterpret_cast<Entry *>(b.workspace + l.entry),
+            GRAD ? reinterpret_cast<float *>(b.workspace + l.share) : nullptr,
+            !GRAD && l.tiles ? reinterpret_cast<uint16_t *>(b.workspace + l.strip) : nullptr, l.strips);
+    };
+    if (l.entries <= 64) go(std::integral_constant<int, 64>());
+    else if (l.entries <= 256) go(std::integral_constant<int, 256>());
+    else go(std::integral_constant<int, kMostEntries>());
     return hipGetLastError();
 }
 
@@ -216,19 +314,28 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
 {
     const HeadBuffers h = head_of(l, b);
     const Teacher teacher = teacher_of(l, b);
-    const Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
-    hipError_t error = calls.direct() ? hipSuccess : mark(l, b, stream);
+    Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
+    const bool direct = calls.direct(), tiles = !direct && l.tiles;
+    hipError_t error = direct ? hipSuccess : rows<false>(l, b, stream);
+    if (tiles) {
+        calls.tokens_of_rows = calls.template at<int32_t>(l.token);
+        calls.picks = Tempered::Picks{calls.template at<uint16_t>(l.strip), calls.template at<Entry>(l.entry), calls.tokens_of_rows, picked, l.strips, l.entries};
+    }
     const int side = calls.loss_parts();
     const int64_t parts = (l.head.vocab + side - 1) / side;
+    const int32_t *const place = direct ? nullptr : calls.template at<int32_t>(l.head.place);
+    const float2 *const stats = calls.template at<float2>(l.head.stats);
     const auto join = [&](auto waves) {
         constexpr int WAVES = decltype(waves)::value;
         join_divergence<T, WAVES><<<dim3(uint32_t(l.head.tokens)), 64 * WAVES, 0, stream>>>(
-            teacher, calls.direct() ? nullptr : calls.template at<int32_t>(l.head.place), parts, l.head.parts, calls.template at<float2>(l.head.stats),
-            static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.head.width, loss, lse, picked);
-        calls.launched();
+            teacher, place, parts, l.head.parts, stats, static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.head.width, loss, lse,
+            picked);
     };
-    if (calls.direct()) join(std::integral_constant<int, 16>());
+    if (tiles)
+        join_picked<<<dim3(uint32_t((l.head.tokens + 3) / 4)), 256, 0, stream>>>(teacher, l.head.tokens, place, parts, l.head.parts, stats, loss, lse, picked);
+    else if (direct) join(std::integral_constant<int, 16>());
     else join(std::integral_constant<int, 4>());
+    calls.launched();
     if (error == hipSuccess) error = calls.error;
     return error;
 }
@@ -238,16 +345,18 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
                        void *dweight, hipStream_t stream)
 {
     const HeadBuffers h = head_of(l, b);
-    const Teacher teacher = teacher_of(l, b);
-    const Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
-    const hipError_t marked = l.head.tokens ? mark(l, b, stream) : hipSuccess;
-    const hipError_t rest = calls.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), teacher.inverse, [&](int64_t first, int64_t columns) {
-        delta_entries<T><<<dim3(uint32_t((l.head.tokens + kEntryWaves - 1) / kEntryWaves)), 64 * kEntryWaves, 0, stream>>>(
-            teacher, calls.template at<int32_t>(l.head.place), l.head.tokens, calls.template at<float>(l.head.lse),
-            calls.template at<float>(l.head.factor), picked, first, columns, calls.template at<T>(l.head.delta), l.head.piece);
+    const float inverse = teacher_of(l, b).inverse;
+    const Calls<T, Tempered> calls{l.head, h, stream, Tempered{inverse}};
+    hipError_t error = l.head.tokens ? rows<true>(l, b, stream) : hipSuccess;
+    const int64_t all = l.head.tokens * l.entries;
+    const hipError_t rest = calls.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), inverse, [&](int64_t first, int64_t columns) {
+        delta_entries<T><<<dim3(uint32_t((all + 255) / 256)), 256, 0, stream>>>(
+            calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
+            calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns,
+            calls.template at<T>(l.head.delta), l.head.piece);
         calls.launched();
     });
-    return marked != hipSuccess ? marked : rest;
+    return error != hipSuccess ? error : rest;
 }
 
 }  // namespace

@@ -25,13 +25,31 @@ struct Header {
     float unscale;           // what the products of d are multiplied by
 };
 
-// What the softmax is taken of: the logits, with one target a row; or the logits over a temperature, with targets elsewhere.
+// What the softmax is taken of: the logits, with one target a row; or the logits over a temperature, where a row has a teacher's entries
+// instead (which cgx_distill.hip takes care of, but for the logits that a call's tiles pick out for it).
 struct Targets {
-    static constexpr bool kPicks = true;                 // a row's target is looked for in its tiles
+    static constexpr bool kTargets = true;
+    struct Picks {};
     static __device__ __forceinline__ float of(float z) { return z; }
 };
+
+// The entries of a row, sorted by id: where those of each 64 columns of the vocabulary begin (10 bits) and how many they are (6 bits; 63: or
+// more).  A wave's tile is 64 columns wide, so a lane learns from one load whether its row has any there.
+constexpr int kStripColumns = 64, kStripBits = 10;
+constexpr uint32_t kStripMost = 63;
+struct Entry {
+    int32_t id, place;                                   // id, and the entry's place in its row
+};
 struct Tempered {
-    static constexpr bool kPicks = false;
+    static constexpr bool kTargets = false;
+    struct Picks {
+        const uint16_t *strips = nullptr;                // [tokens][pitch], or null: nothing is picked
+        const Entry *entries = nullptr;                  // [tokens][count]
+        const int32_t *token = nullptr;                  // of a row
+        float *picked = nullptr;                         // [tokens][count]
+        int64_t pitch = 0;
+        int32_t count = 0;
+    };
     float inverse;                                       // 1 / temperature
     __device__ __forceinline__ float of(float z) const { return z * inverse; }
 };
@@ -73,6 +91,7 @@ constexpr int kListThreads = 1024, kListWaves = kListThreads / 64, kListEach = 8
 struct Lists {
     int32_t *place, *target;
     float *base, *factor;
+    int32_t *token;          // of a row; or null
 };
 template <typename T>
 struct Padding {
@@ -201,6 +220,7 @@ __global__ __launch_bounds__(kListThreads) void list_tokens(const int64_t *__res
                 const bool outside = v < 0 || v >= vocab;
                 listed[before] = int32_t(at - from);
                 lists.target[row] = outside ? -1 : int32_t(v);
+                if (lists.token) lists.token[row] = int32_t(at);
                 if (dloss) {
                     lists.base[row] = lse[at];
                     lists.factor[row] = outside ? __builtin_nanf("") : top_bits ? ldexpf(dloss[at] / unit, top_bits - kLift) : dloss[at];
@@ -258,6 +278,73 @@ __device__ __forceinline__ uint32_t up(int64_t v, int to) { return uint32_t((v +
 template <typename K>
 using Lds = unsigned char[K::kLds];
 
+// Picks a tile's logits at its rows' entries.  The loads it depends on, one after another, are spread over the tile's end: where a row's entries
+// are when it begins, the first of them half way through the exponentials; most rows of a tile's 64 columns have none or one.
+template <typename K, typename S>
+struct Picker {
+    __device__ __forceinline__ Picker(const typename S::Picks &, const K &, const Tokens &, int64_t, int64_t, int64_t) {}
+    __device__ __forceinline__ void fetch(const typename S::Picks &) {}
+    __device__ __forceinline__ void put(const typename S::Picks &, const K &) {}
+};
+template <typename K>
+struct Picker<K, Tempered> {
+    using Picks = Tempered::Picks;
+    static_assert(K::TN * 16 == kStripColumns, "a wave's columns are a strip");
+    uint32_t at[K::TM];
+    int32_t token[K::TM], column;
+    Entry entry[K::TM];
+    // first: the tile's first column in the vocabulary.
+    __device__ __forceinline__ Picker(const Picks &picks, const K &tile, const Tokens &tokens, int64_t m0, int64_t count, int64_t first)
+    {
+        if (!picks.strips) return;
+        const int64_t strip = (first + tile.wn) / kStripColumns;
+        column = int32_t(strip * kStripColumns);
+#pragma unroll
+        for (int i = 0; i < K::TM; i++) {
+            const int64_t row = m0 + tile.wm + 16 * i + (tile.lane & 15);
+            const bool none = row >= count || column >= tokens.vocab;          // (tiles go over both ends)
+            token[i] = none ? 0 : count == tokens.tokens ? int32_t(row) : picks.token[row];
+            at[i] = none ? 0 : picks.strips[token[i] * picks.pitch + strip];
+        }
+    }
+    __device__ __forceinline__ void fetch(const Picks &picks)
+    {
+        if (!picks.strips) return;
+#pragma unroll
+        for (int i = 0; i < K::TM; i++)
+            if (at[i] >> kStripBits) entry[i] = picks.entries[int64_t(token[i]) * picks.count + (at[i] & ((1u << kStripBits) - 1))];
+    }
+    __device__ __forceinline__ void put(const Picks &picks, const K &tile)
+    {
+        if (!picks.strips) return;
+        const int32_t c0 = column + 16 * (tile.lane >> 4);
+#pragma unroll
+        for (int i = 0; i < K::TM; i++) {
+            uint32_t left = at[i] >> kStripBits, from = at[i] & ((1u << kStripBits) - 1);
+            const bool more = left == kStripMost;
+            const Entry *const row = picks.entries + int64_t(token[i]) * picks.count;
+            Entry e = entry[i];
+            while (left) {
+                const int32_t d = e.id - c0;
+                if (d >= 0 && d < 16) {
+                    float z = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 16; k++)
+                        if (d == k) z = tile.acc[i][k / 4][k % 4];
+                    picks.picked[int64_t(token[i]) * picks.count + e.place] = z;
+                }
+                left--;
+                from++;
+                if (left) e = row[from];
+                else if (more && from < uint32_t(picks.count)) {
+                    e = row[from];
+                    left = e.id < column + kStripColumns;
+                }
+            }
+        }
+    }
+};
+
 // Logits of a tile, and what its rows add to their softmax: the largest logit m, the sum of exp(logit - m), in binary32; parts join by
 // m = max m_k, sum = sum_k sum_k exp(m_k - m), so that no logit is ever stored.  A lane holds 16 neighbouring columns of a row (strips),
 // so a row's maximum and sum take two exchanges between lanes and one between waves.
@@ -269,7 +356,7 @@ using Lds = unsigned char[K::kLds];
 template <typename K, typename S>
 __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                           int64_t pitch, int64_t first, int64_t columns, int64_t parts,
-                                                          float2 *__restrict__ stats, float *__restrict__ picked, S softmax)
+                                                          float2 *__restrict__ stats, float *__restrict__ picked, S softmax, typename S::Picks picks)
 {
     using T = typename K::T;
     __shared__ __align__(256) Lds<K> lds;
@@ -289,11 +376,13 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
     const int g = tile.lane >> 4, r = tile.lane & 15, wave_n = tile.wave % K::WN;
     const int64_t c0 = n0 + tile.wn + 16 * g;
     const bool whole = n0 + K::BN <= columns;
+    Picker<K, S> picker(picks, tile, tokens, m0, count, first + n0);
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
+        if (i == K::TM / 2) picker.fetch(picks);
         const int m = tile.wm + 16 * i + r;
         const int64_t row = m0 + m;
-        if (S::kPicks && row < count) {
+        if (S::kTargets && row < count) {
             const int64_t d = int64_t(tokens.target_of(row)) - first - c0;
             if (d >= 0 && d < 16) {
 #pragma unroll
@@ -308,22 +397,23 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
         for (int j = 0; j < K::TN; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                tile.acc[i][j][e] = softmax.of(tile.acc[i][j][e]);
                 if (!whole && c0 + 4 * j + e >= columns) tile.acc[i][j][e] = -__builtin_inff();
                 top = fmaxf(top, tile.acc[i][j][e]);
             }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = softmax.of(top);                           // (a positive factor: the largest stays the largest)
         const float from = top == -__builtin_inff() ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < K::TN; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) sum += exp_from<T>(tile.acc[i][j][e], from);
+            for (int e = 0; e < 4; e++) sum += exp_from<T>(softmax.of(tile.acc[i][j][e]), from);
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
         if (g == 0) joined[wave_n * K::BM + m] = float2{top, sum};
     }
+    picker.put(picks, tile);
     __syncthreads();
     for (int m = int(threadIdx.x); m < K::BM; m += K::kThreads) {
         if (m0 + m >= count) break;
@@ -431,14 +521,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
     // a token's columns: kLanes neighbouring lanes, kEach columns a lane
     constexpr int kEach = 16 * kFewColumns / (64 * kFewWaves), kLanes = kFewColumns / kEach;
     const int m = tid / kLanes, first = tid % kLanes * kEach;
-    const int32_t target = S::kPicks && m < count ? tokens.target_of(m0 + m) : -1;
+    const int32_t target = S::kTargets && m < count ? tokens.target_of(m0 + m) : -1;
     float z[kEach], top = -__builtin_inff();
 #pragma unroll
     for (int e = 0; e < kEach; e++) {
         z[e] = 0.f;
 #pragma unroll
         for (int k = 0; k < kFewWaves; k++) z[e] += part[k][m][first + e];
-        if (S::kPicks && m < count && target == n0 + first + e) picked[m0 + m] = z[e];
+        if (S::kTargets && m < count && target == n0 + first + e) picked[m0 + m] = z[e];
         z[e] = softmax.of(z[e]);
         if (first + e >= columns) z[e] = -__builtin_inff();
         top = fmaxf(top, z[e]);
@@ -562,7 +652,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
         const int64_t row = m0 + tile.wm + 16 * i + r;
         const bool counts = row < count;
         const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] : 0.f;
-        const int64_t hit = S::kPicks && counts ? int64_t(target[row]) - first - c0 : -1;
+        const int64_t hit = S::kTargets && counts ? int64_t(target[row]) - first - c0 : -1;
         T *const out = delta + row * piece + c0;
 #pragma unroll
         for (int k = 0; k < 16; k += kPer) {
@@ -575,7 +665,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
                     if (!counts || c0 + k + e >= columns) v[e] = T(0.f);
             *reinterpret_cast<Vec *>(out + k) = v;
         }
-        if (S::kPicks && hit >= 0 && hit < 16) {
+        if (S::kTargets && hit >= 0 && hit < 16) {
             float z = 0.f;
 #pragma unroll
             for (int k = 0; k < 16; k++)
@@ -835,6 +925,8 @@ struct Calls {
     const HeadBuffers &b;
     hipStream_t stream;
     S softmax = S();
+    typename S::Picks picks = typename S::Picks();
+    int32_t *tokens_of_rows = nullptr;
     mutable hipError_t error = hipSuccess;      // of the first launch that was refused
 
     void launched() const
@@ -868,7 +960,7 @@ struct Calls {
         list_tokens<T><<<dim3(uint32_t(grid + pads)), kListThreads, 0, stream>>>(
             b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, l.dt == CGX_F16 ? 14 : l.dt == CGX_BF16 ? kLift : 0,
             outer, static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, int32_t(head_depth(l.dt)), h.own ? 1 : 0, header(),
-            Lists{at<int32_t>(l.place), at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor)}, uint32_t(grid),
+            Lists{at<int32_t>(l.place), at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), tokens_of_rows}, uint32_t(grid),
             Padding<T>{static_cast<const T *>(b.weight), at<T>(l.weight), columns, l.width, l.pitch});
         launched();
     }
@@ -889,7 +981,7 @@ struct Calls {
     {
         loss_tiles<K, S><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
             tokens(), direct() ? Hidden<T>{static_cast<const T *>(b.hidden), nullptr, l.tokens} : hidden(), weight(first, columns), l.pitch,
-            first, columns, l.parts, at<float2>(l.stats), at<float>(l.picked), softmax);
+            first, columns, l.parts, at<float2>(l.stats), at<float>(l.picked), softmax, picks);
         launched();
     }
     void loss_of_few() const
