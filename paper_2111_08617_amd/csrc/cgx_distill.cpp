@@ -21,7 +21,7 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     };
     l.mark = take(tokens * 8);
     l.token = take(tokens * 4);
-    l.entry = take(tokens * entries * 8);
+    l.entry = take(tokens * entries * 8 + 16);           // (they are read in pairs)
     // the shares are the gradient call's, the strips the loss's
     const size_t shared = at;
     size_t end = at;

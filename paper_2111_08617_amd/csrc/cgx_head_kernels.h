@@ -278,21 +278,26 @@ __device__ __forceinline__ uint32_t up(int64_t v, int to) { return uint32_t((v +
 template <typename K>
 using Lds = unsigned char[K::kLds];
 
-// Picks a tile's logits at its rows' entries.  The loads it depends on, one after another, are spread over the tile's end: where a row's entries
-// are when it begins, the first of them half way through the exponentials; most rows of a tile's 64 columns have none or one.
+// Picks a tile's logits at its rows' entries.  Most rows have no entry among a wave's 64 columns, or one, anywhere, and registers have no index: so
+// a wave that has any puts its logits into LDS, as many rows as its share of that holds, and each lane looks up one row's.  The loads that depend on each
+// other are spread over the tile's end: where a row's entries are when it begins, the first two of them half way through the exponentials.
 template <typename K, typename S>
 struct Picker {
     __device__ __forceinline__ Picker(const typename S::Picks &, const K &, const Tokens &, int64_t, int64_t, int64_t) {}
     __device__ __forceinline__ void fetch(const typename S::Picks &) {}
-    __device__ __forceinline__ void put(const typename S::Picks &, const K &) {}
+    __device__ __forceinline__ void put(const typename S::Picks &, const K &, unsigned char *) {}
 };
 template <typename K>
 struct Picker<K, Tempered> {
     using Picks = Tempered::Picks;
-    static_assert(K::TN * 16 == kStripColumns, "a wave's columns are a strip");
-    uint32_t at[K::TM];
-    int32_t token[K::TM], column;
-    Entry entry[K::TM];
+    static constexpr int kRowBytes = kStripColumns * 4, kShare = K::kLds / (K::WM * K::WN);
+    static constexpr int kRows = 16 * K::TM < kShare / kRowBytes ? 16 * K::TM : kShare / kRowBytes, kRounds = 16 * K::TM / kRows;
+    static_assert(K::TN * 16 == kStripColumns && kRows % 16 == 0 && kRows <= 64 && kRows * kRounds == 16 * K::TM, "a strip's rows in whole rounds");
+    typedef int32_t Pair __attribute__((ext_vector_type(4)));              // two entries
+    typedef Pair Anywhere __attribute__((aligned(8)));
+    uint32_t at[kRounds];
+    int32_t token[kRounds], column;
+    Pair pair[kRounds];
     // first: the tile's first column in the vocabulary.
     __device__ __forceinline__ Picker(const Picks &picks, const K &tile, const Tokens &tokens, int64_t m0, int64_t count, int64_t first)
     {
@@ -300,47 +305,62 @@ struct Picker<K, Tempered> {
         const int64_t strip = (first + tile.wn) / kStripColumns;
         column = int32_t(strip * kStripColumns);
 #pragma unroll
-        for (int i = 0; i < K::TM; i++) {
-            const int64_t row = m0 + tile.wm + 16 * i + (tile.lane & 15);
-            const bool none = row >= count || column >= tokens.vocab;          // (tiles go over both ends)
-            token[i] = none ? 0 : count == tokens.tokens ? int32_t(row) : picks.token[row];
-            at[i] = none ? 0 : picks.strips[token[i] * picks.pitch + strip];
+        for (int q = 0; q < kRounds; q++) {
+            const int64_t row = m0 + tile.wm + q * kRows + tile.lane;
+            const bool none = tile.lane >= kRows || row >= count || column >= tokens.vocab;      // (tiles go over both ends)
+            token[q] = none ? 0 : count == tokens.tokens ? int32_t(row) : picks.token[row];
+            at[q] = none ? 0 : picks.strips[token[q] * picks.pitch + strip];
         }
     }
+    __device__ __forceinline__ static const Entry *row_of(const Picks &picks, int32_t token) { return picks.entries + int64_t(token) * picks.count; }
+    // (the array is padded by two entries)
+    __device__ __forceinline__ static Pair load(const Entry *p) { return *reinterpret_cast<const Anywhere *>(p); }
     __device__ __forceinline__ void fetch(const Picks &picks)
     {
         if (!picks.strips) return;
 #pragma unroll
-        for (int i = 0; i < K::TM; i++)
-            if (at[i] >> kStripBits) entry[i] = picks.entries[int64_t(token[i]) * picks.count + (at[i] & ((1u << kStripBits) - 1))];
+        for (int q = 0; q < kRounds; q++)
+            if (at[q] >> kStripBits) pair[q] = load(row_of(picks, token[q]) + (at[q] & ((1u << kStripBits) - 1)));
     }
-    __device__ __forceinline__ void put(const Picks &picks, const K &tile)
+    static __device__ __forceinline__ void fence()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // (LDS accesses of a wave are in order)
+        __builtin_amdgcn_wave_barrier();
+    }
+    // lds: what the whole block is done with.  Its 16-byte pieces are permuted within a row, so that neighbouring rows' fall on different banks.
+    __device__ __forceinline__ void put(const Picks &picks, const K &tile, unsigned char *lds)
     {
         if (!picks.strips) return;
-        const int32_t c0 = column + 16 * (tile.lane >> 4);
+        unsigned char *const own = lds + tile.wave * kShare;
+        const int g = tile.lane >> 4, r = tile.lane & 15;
 #pragma unroll
-        for (int i = 0; i < K::TM; i++) {
-            uint32_t left = at[i] >> kStripBits, from = at[i] & ((1u << kStripBits) - 1);
+        for (int q = 0; q < kRounds; q++) {
+            uint32_t left = at[q] >> kStripBits;
+            if (!__ballot(left != 0)) continue;
+#pragma unroll
+            for (int i = 0; i < kRows / 16; i++)
+#pragma unroll
+                for (int j = 0; j < K::TN; j++)
+                    *reinterpret_cast<f32x4 *>(own + (16 * i + r) * kRowBytes + (((4 * g + j) ^ r) << 4)) = tile.acc[q * (kRows / 16) + i][j];
+            fence();
+            uint32_t from = at[q] & ((1u << kStripBits) - 1);
             const bool more = left == kStripMost;
-            const Entry *const row = picks.entries + int64_t(token[i]) * picks.count;
-            Entry e = entry[i];
+            if (more) left = uint32_t(picks.count) - from;       // (up to the end of the row, or of the strip)
+            const Entry *const row = row_of(picks, token[q]);
+            float *const out = picks.picked + int64_t(token[q]) * picks.count;
+            const auto logit = [&](int32_t d) { return *reinterpret_cast<const float *>(own + tile.lane * kRowBytes + (((d >> 2) ^ r) << 4) + (d & 3) * 4); };
+            Pair e = pair[q];
             while (left) {
-                const int32_t d = e.id - c0;
-                if (d >= 0 && d < 16) {
-                    float z = 0.f;
-#pragma unroll
-                    for (int k = 0; k < 16; k++)
-                        if (d == k) z = tile.acc[i][k / 4][k % 4];
-                    picks.picked[int64_t(token[i]) * picks.count + e.place] = z;
-                }
-                left--;
-                from++;
-                if (left) e = row[from];
-                else if (more && from < uint32_t(picks.count)) {
-                    e = row[from];
-                    left = e.id < column + kStripColumns;
-                }
+                const Pair next = left > 2 ? load(row + from + 2) : e;
+                const int32_t d = e[0] - column, d2 = e[2] - column;
+                if (d >= 0 && d < kStripColumns) out[e[1]] = logit(d);
+                if (left > 1 && d2 >= 0 && d2 < kStripColumns) out[e[3]] = logit(d2);
+                if (left <= 2 || (more && d2 >= kStripColumns)) break;
+                left -= 2;
+                from += 2;
+                e = next;
             }
+            fence();
         }
     }
 };
@@ -413,7 +433,6 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
         sum += __shfl_xor(sum, 32, 64);
         if (g == 0) joined[wave_n * K::BM + m] = float2{top, sum};
     }
-    picker.put(picks, tile);
     __syncthreads();
     for (int m = int(threadIdx.x); m < K::BM; m += K::kThreads) {
         if (m0 + m >= count) break;
@@ -426,6 +445,8 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
         for (int w = 0; w < K::WN; w++) sum += joined[w * K::BM + m].y * __builtin_amdgcn_exp2f((joined[w * K::BM + m].x - from) * kLog2e);
         stats[(m0 + m) * parts + (first + n0) / K::BN] = float2{top, sum};
     }
+    if constexpr (!S::kTargets) __syncthreads();
+    picker.put(picks, tile, lds);
 }
 
 // The same for few tokens, where reading W is all that takes time, and for few logits: a block per 16 tokens and kFewColumns rows of W, whose four waves each sum a
