@@ -12,7 +12,7 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     l.entries = entries;
     // (with more entries than this in every 64 columns a tile's end would take longer than the tile)
     l.tiles = int64_t(entries) * 64 <= 4 * vocab;
-    l.strips = (vocab + 127) / 128 * 2;
+    l.strips = (vocab + 511) / 512 * 8;
     size_t at = l.head.bytes;
     const auto take = [&at](int64_t bytes) {
         const size_t here = at;

@@ -12,7 +12,7 @@ struct DistillLayout {
     HeadLayout head;
     int32_t entries = 0;
     bool tiles = false;      // the loss picks the student's logits out of the tiles they are formed in
-    int64_t strips = 0;      // of 64 columns of the vocabulary, rounded up to an even number
+    int64_t strips = 0;      // of 64 columns of the vocabulary, rounded up to a multiple of 8
     size_t mark = 0;         // int64 [tokens]: what the head's list reads as targets: kTakesPart, kNoPart or (kWrong) not a number
     size_t token = 0;        // int32 [tokens]: of a row of the list
     size_t entry = 0;        // Entry [tokens][entries]: sorted by id; those that are none are the last, with an id of -1

@@ -41,19 +41,23 @@ __device__ __forceinline__ TeacherRow teacher_row(const Teacher &t, int64_t toke
     TeacherRow r{-__builtin_inff(), 0.f, false};
     const int64_t first = token * t.entries;
     bool wrong = false;
+    // (one pass over the entries, each lane with a maximum of its own: the loads are what takes time)
     for (int k = lane; k < t.entries; k += 64) {
         const int64_t id = t.ids[first + k];
-        if (id == t.ignore) continue;
         const float x = t.logit(first + k) * t.inverse;
+        if (id == t.ignore) continue;
         wrong |= id < 0 || id >= t.vocab || !(x < __builtin_inff());
-        r.top = fmaxf(r.top, x);
+        const float top = fmaxf(r.top, x);
+        if (top == -__builtin_inff()) continue;
+        r.sum = r.sum * expf(r.top - top) + expf(x - top);
+        r.top = top;
     }
+    float top = r.top;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) r.top = fmaxf(r.top, __shfl_xor(r.top, d, 64));
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     r.wrong = __ballot(wrong) != 0;
-    if (r.top == -__builtin_inff()) return r;
-    for (int k = lane; k < t.entries; k += 64)
-        if (t.ids[first + k] != t.ignore) r.sum += expf(t.logit(first + k) * t.inverse - r.top);
+    r.sum = top == -__builtin_inff() ? 0.f : r.sum * expf(r.top - top);
+    r.top = top;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) r.sum += __shfl_xor(r.sum, d, 64);
     return r;
@@ -135,56 +139,57 @@ __global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, 
         entries[first + k] = e;
     }
     if (GRAD || !strips) return;
-    // (entries that are none come after all strips)
-    const auto begin = [&](int64_t id) {
-        int low = 0;
-#pragma unroll
-        for (int step = M / 2; step > 0; step /= 2)
-            if (s.key[low + step - 1] < uint64_t(id) << kStripBits) low += step;
-        return low + (s.key[low] < uint64_t(id) << kStripBits ? 1 : 0);
-    };
-    const int64_t used = (teacher.vocab + kStripColumns - 1) / kStripColumns;
-    for (int64_t strip = lane; strip < used; strip += 64) {
-        const int from = begin(strip * kStripColumns), to = begin((strip + 1) * kStripColumns), n = to - from;
-        strips[token * pitch + strip] = n ? uint16_t(uint32_t(from) | uint32_t(n < int(kStripMost) ? n : int(kStripMost)) << kStripBits) : uint16_t(0);
+    // (of 8 at a time: rows of strips are whole pieces of 16 bytes)
+    typedef uint32_t Four __attribute__((ext_vector_type(4)));
+    uint16_t *const row = strips + token * pitch;
+    for (int64_t strip = lane * 8; strip < pitch; strip += 512) *reinterpret_cast<Four *>(row + strip) = Four(0u);
+    wave_fence();
+    // the first entry of a strip writes it, after the zeros: stores of a wave to one address are in order
+    const auto strip_of = [](uint64_t key) { return int64_t(key >> kStripBits) / kStripColumns; };
+    for (int k = lane; k < teacher.entries; k += 64) {
+        const uint64_t key = s.key[k];
+        if (key == kNone || (k > 0 && strip_of(s.key[k - 1]) == strip_of(key))) continue;
+        uint32_t n = 1;
+        while (n < kStripMost && k + int(n) < teacher.entries && s.key[k + n] != kNone && strip_of(s.key[k + n]) == strip_of(key)) n++;
+        row[strip_of(key)] = uint16_t(uint32_t(k) | n << kStripBits);
     }
 }
 
-// 16 bytes of a row that starts at any element, as binary32.
-template <typename T>
-struct Slice {
-    static constexpr int V = 16 / int(sizeof(T));
-    float v[V];
-    __device__ __forceinline__ void load(const T *row, int64_t column, int64_t width)
-    {
-        typedef T Vec __attribute__((ext_vector_type(V)));
-        typedef Vec Anywhere __attribute__((aligned(sizeof(T))));
-        if (column + V <= width) {
-            const Vec x = *reinterpret_cast<const Anywhere *>(row + column);
-#pragma unroll
-            for (int e = 0; e < V; e++) v[e] = float(x[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; e++) v[e] = column + e < width ? float(row[column + e]) : 0.f;
-        }
-    }
-};
-
-// The loss from the tiles' parts of a token's softmax and its picked logits: a wave per token.
-__global__ __launch_bounds__(256) void join_picked(Teacher teacher, int64_t tokens, const int32_t *__restrict__ place, int64_t parts, int64_t pitch,
-                                                   const float2 *__restrict__ stats, float *__restrict__ loss, float *__restrict__ lse,
-                                                   float *__restrict__ picked)
+// A sum over the lanes of WAVES waves, in a fixed order; in the first of them.
+template <int WAVES>
+__device__ __forceinline__ float lanes_sum(float v, int lane)
 {
-    const int lane = int(threadIdx.x) & 63;
-    const int64_t token = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (token >= tokens) return;
-    const TeacherRow row = teacher_row(teacher, token, lane);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    if constexpr (WAVES > 1) {
+        __shared__ float waves[WAVES];
+        if ((lane & 63) == 0) waves[lane >> 6] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) v += waves[w];
+    }
+    return v;
+}
+
+// The loss from the parts of a token's softmax and its picked logits: a wave per token, four of them in a block, or (few tokens) a block of many waves
+// per token.
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_picked(Teacher teacher, int64_t tokens, const int32_t *__restrict__ place,
+                                                                               int64_t parts, int64_t pitch, const float2 *__restrict__ stats,
+                                                                               float *__restrict__ loss, float *__restrict__ lse, float *__restrict__ picked)
+{
+    constexpr int kLanes = 64 * WAVES;
+    const int lane = int(threadIdx.x) % kLanes;
+    const int64_t token = int64_t(blockIdx.x) * join_tokens<WAVES> + threadIdx.x / kLanes;
+    if (token >= tokens) return;                         // (a whole wave; for WAVES > 1 no block)
+    const TeacherRow row = teacher_row(teacher, token, lane & 63);
     const int64_t first = token * teacher.entries;
     const bool takes_part = row.takes_part();
-    const float total = takes_part ? log_sum<1>(stats + int64_t(place[token]) * pitch, parts, lane) : 0.f;
+    const float total = takes_part ? log_sum<WAVES>(stats + (place ? int64_t(place[token]) : token) * pitch, parts, lane) : 0.f;
     const float log_mass = row.top + logf(row.sum);
     float sum = 0.f;
-    for (int k = lane; k < teacher.entries; k += 64) {
+    for (int k = lane; k < teacher.entries; k += kLanes) {
         const int64_t id = teacher.ids[first + k];
         if (!takes_part || id == teacher.ignore) picked[first + k] = 0.f;
         else if (id < 0 || id >= teacher.vocab) picked[first + k] = __builtin_nanf("");
@@ -193,73 +198,42 @@ __global__ __launch_bounds__(256) void join_picked(Teacher teacher, int64_t toke
             if (q > 0.f) sum += q * (scaled - log_mass + total - picked[first + k] * teacher.inverse);
         }
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    sum = lanes_sum<WAVES>(sum, lane);
     if (lane != 0) return;
     lse[token] = total;
     loss[token] = !takes_part ? 0.f : row.wrong ? __builtin_nanf("") : sum;
 }
 
-// Joins the parts of a token's softmax, takes the student's logits at the teacher's entries (a wave per entry, four at a time), and the divergence.
-// A block of WAVES waves per token.
-constexpr int kDots = 4;
-template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void join_divergence(Teacher teacher, const int32_t *__restrict__ place, int64_t parts, int64_t pitch,
-                                                              const float2 *__restrict__ stats, const T *__restrict__ hidden,
-                                                              const T *__restrict__ weight, int64_t width, float *__restrict__ loss,
-                                                              float *__restrict__ lse, float *__restrict__ picked)
+// The same where no logits were picked: a block per token takes the products of its entries' rows, a wave kDots of them.
+constexpr int kGatherWaves = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * kGatherWaves) void join_gathered(Teacher teacher, const int32_t *__restrict__ place, int64_t parts, int64_t pitch,
+                                                                   const float2 *__restrict__ stats, const T *__restrict__ hidden,
+                                                                   const T *__restrict__ weight, int64_t width, float *__restrict__ loss,
+                                                                   float *__restrict__ lse, float *__restrict__ picked)
 {
-    __shared__ float sums[WAVES];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t token = blockIdx.x;
+    const int64_t token = blockIdx.x, first = token * teacher.entries;
     const TeacherRow row = teacher_row(teacher, token, lane);
-    const int64_t first = token * teacher.entries;
     if (!row.takes_part()) {                             // (the same in all waves)
-        for (int k = tid; k < teacher.entries; k += 64 * WAVES) picked[first + k] = 0.f;
+        for (int k = tid; k < teacher.entries; k += 64 * kGatherWaves) picked[first + k] = 0.f;
         if (tid == 0) loss[token] = lse[token] = 0.f;
         return;
     }
-    const float total = log_sum<WAVES>(stats + (place ? int64_t(place[token]) : token) * pitch, parts, tid);
+    const float total = log_sum<kGatherWaves>(stats + (place ? int64_t(place[token]) : token) * pitch, parts, tid);
     const float log_mass = row.top + logf(row.sum);
-    const T *const x = hidden + token * width;
     float sum = 0.f;
-    for (int k0 = wave * kDots; k0 < teacher.entries; k0 += WAVES * kDots) {
-        int64_t id[kDots];
-        bool inside[kDots];
-        float dot[kDots];
-#pragma unroll
-        for (int k = 0; k < kDots; k++) {
-            id[k] = k0 + k < teacher.entries ? teacher.ids[first + k0 + k] : teacher.ignore;
-            inside[k] = id[k] != teacher.ignore && id[k] >= 0 && id[k] < teacher.vocab;
-            dot[k] = 0.f;
-        }
-        for (int64_t column = lane * Slice<T>::V; column < width; column += 64 * Slice<T>::V) {
-            Slice<T> a, b[kDots];
-            a.load(x, column, width);
-#pragma unroll
-            for (int k = 0; k < kDots; k++) b[k].load(weight + (inside[k] ? id[k] : 0) * width, column, width);
-#pragma unroll
-            for (int k = 0; k < kDots; k++)
-#pragma unroll
-                for (int e = 0; e < Slice<T>::V; e++) dot[k] = __builtin_fmaf(a.v[e], b[k].v[e], dot[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kDots; k++) {
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) dot[k] += __shfl_xor(dot[k], d, 64);
-            if (k0 + k >= teacher.entries) continue;
-            const bool marked = id[k] == teacher.ignore;
-            if (lane == 0) picked[first + k0 + k] = marked ? 0.f : inside[k] ? dot[k] : __builtin_nanf("");
-            if (marked) continue;
-            const float scaled = teacher.logit(first + k0 + k) * teacher.inverse, q = row.share(scaled);
-            if (q > 0.f) sum += q * (scaled - log_mass + total - dot[k] * teacher.inverse);
-        }
-    }
-    if (lane == 0) sums[wave] = sum;
-    __syncthreads();
+    for (int k0 = wave * kDots; k0 < teacher.entries; k0 += kGatherWaves * kDots)
+        entry_dots(hidden + token * width, weight, width, teacher.vocab, teacher.ids + first, teacher.ignore, k0, teacher.entries, lane,
+                   [&](int k, int64_t id, bool inside, float z) {
+                       if (lane != 0) return;
+                       picked[first + k] = id == teacher.ignore ? 0.f : inside ? z : __builtin_nanf("");
+                       if (id == teacher.ignore) return;
+                       const float scaled = teacher.logit(first + k) * teacher.inverse, q = row.share(scaled);
+                       if (q > 0.f) sum += q * (scaled - log_mass + total - z * teacher.inverse);
+                   });
+    sum = lanes_sum<kGatherWaves>(sum, tid);
     if (tid != 0) return;
-    sum = 0.f;
-    for (int w = 0; w < WAVES; w++) sum += sums[w];
     lse[token] = total;
     loss[token] = row.wrong ? __builtin_nanf("") : sum;
 }
@@ -299,6 +273,7 @@ hipError_t rows(const DistillLayout &l, const DistillBuffers &b, hipStream_t str
             !GRAD && l.tiles ? reinterpret_cast<uint16_t *>(b.workspace + l.strip) : nullptr, l.strips);
     };
     if (l.entries <= 64) go(std::integral_constant<int, 64>());
+    else if (l.entries <= 128) go(std::integral_constant<int, 128>());
     else if (l.entries <= 256) go(std::integral_constant<int, 256>());
     else go(std::integral_constant<int, kMostEntries>());
     return hipGetLastError();
@@ -315,26 +290,37 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
     const HeadBuffers h = head_of(l, b);
     const Teacher teacher = teacher_of(l, b);
     Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
-    const bool direct = calls.direct(), tiles = !direct && l.tiles;
+    // Few tokens' kernel takes the products of the entries' rows along; tiles pick the logits out; the rest (17 to 64 tokens as they come, and so
+    // many entries that most columns are some) is gathered afterwards.
+    const bool direct = calls.direct(), few = calls.few(), tiles = !direct && l.tiles;
     hipError_t error = direct ? hipSuccess : rows<false>(l, b, stream);
-    if (tiles) {
+    if (few) {
+        calls.picks.blocks = uint32_t((l.head.tokens * ((l.entries + kDots - 1) / kDots) + kFewWaves - 1) / kFewWaves);
+        calls.picks.ids = b.ids;
+        calls.picks.ignore = b.ignore;
+    } else if (tiles) {
         calls.tokens_of_rows = calls.template at<int32_t>(l.token);
-        calls.picks = Tempered::Picks{calls.template at<uint16_t>(l.strip), calls.template at<Entry>(l.entry), calls.tokens_of_rows, picked, l.strips, l.entries};
+        calls.picks.strips = calls.template at<uint16_t>(l.strip);
+        calls.picks.entries = calls.template at<Entry>(l.entry);
+        calls.picks.token = calls.tokens_of_rows;
+        calls.picks.pitch = l.strips;
     }
+    calls.picks.picked = picked;
+    calls.picks.count = l.entries;
     const int side = calls.loss_parts();
     const int64_t parts = (l.head.vocab + side - 1) / side;
     const int32_t *const place = direct ? nullptr : calls.template at<int32_t>(l.head.place);
     const float2 *const stats = calls.template at<float2>(l.head.stats);
     const auto join = [&](auto waves) {
-        constexpr int WAVES = decltype(waves)::value;
-        join_divergence<T, WAVES><<<dim3(uint32_t(l.head.tokens)), 64 * WAVES, 0, stream>>>(
-            teacher, place, parts, l.head.parts, stats, static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.head.width, loss, lse,
-            picked);
+        constexpr int WAVES = decltype(waves)::value, kPerBlock = join_tokens<WAVES>;
+        join_picked<WAVES><<<dim3(uint32_t((l.head.tokens + kPerBlock - 1) / kPerBlock)), 64 * WAVES * kPerBlock, 0, stream>>>(
+            teacher, l.head.tokens, place, parts, l.head.parts, stats, loss, lse, picked);
     };
-    if (tiles)
-        join_picked<<<dim3(uint32_t((l.head.tokens + 3) / 4)), 256, 0, stream>>>(teacher, l.head.tokens, place, parts, l.head.parts, stats, loss, lse, picked);
-    else if (direct) join(std::integral_constant<int, 16>());
-    else join(std::integral_constant<int, 4>());
+    if (few) join(std::integral_constant<int, kJoinWaves>());
+    else if (tiles) join(std::integral_constant<int, 1>());
+    else
+        join_gathered<T><<<dim3(uint32_t(l.head.tokens)), 64 * kGatherWaves, 0, stream>>>(
+            teacher, place, parts, l.head.parts, stats, static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.head.width, loss, lse, picked);
     calls.launched();
     if (error == hipSuccess) error = calls.error;
     return error;

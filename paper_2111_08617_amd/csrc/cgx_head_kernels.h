@@ -49,6 +49,9 @@ struct Tempered {
         float *picked = nullptr;                         // [tokens][count]
         int64_t pitch = 0;
         int32_t count = 0;
+        uint32_t blocks = 0;                             // few tokens: the first so many blocks take the products of entries' rows
+        const int64_t *ids = nullptr;                    // [tokens][count]
+        int64_t ignore = 0;
     };
     float inverse;                                       // 1 / temperature
     __device__ __forceinline__ float of(float z) const { return z * inverse; }
@@ -449,6 +452,58 @@ __global__ __launch_bounds__(K::kThreads, 2) void loss_tiles(Tokens tokens, Hidd
     picker.put(picks, tile, lds);
 }
 
+// The student's logits at some entries of a token, by a wave: the products of its hidden state and the weight's rows, kDots rows on their way at a
+// time.  `out(k, id, inside, z)` is called by all lanes.
+template <typename T>
+struct Slice {               // 16 bytes of a row that starts at any element, as binary32
+    static constexpr int V = 16 / int(sizeof(T));
+    float v[V];
+    __device__ __forceinline__ void load(const T *row, int64_t column, int64_t width)
+    {
+        typedef T Vec __attribute__((ext_vector_type(V)));
+        typedef Vec Anywhere __attribute__((aligned(sizeof(T))));
+        if (column + V <= width) {
+            const Vec x = *reinterpret_cast<const Anywhere *>(row + column);
+#pragma unroll
+            for (int e = 0; e < V; e++) v[e] = float(x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e++) v[e] = column + e < width ? float(row[column + e]) : 0.f;
+        }
+    }
+};
+constexpr int kDots = 4;
+template <typename T, class Out>
+__device__ __forceinline__ void entry_dots(const T *x, const T *weight, int64_t width, int64_t vocab, const int64_t *ids, int64_t ignore, int from, int count,
+                                           int lane, Out out)
+{
+    int64_t id[kDots];
+    bool inside[kDots];
+    float dot[kDots];
+#pragma unroll
+    for (int k = 0; k < kDots; k++) {
+        id[k] = from + k < count ? ids[from + k] : ignore;
+        inside[k] = id[k] != ignore && id[k] >= 0 && id[k] < vocab;
+        dot[k] = 0.f;
+    }
+    for (int64_t column = lane * Slice<T>::V; column < width; column += 64 * Slice<T>::V) {
+        Slice<T> a, b[kDots];
+        a.load(x, column, width);
+#pragma unroll
+        for (int k = 0; k < kDots; k++) b[k].load(weight + (inside[k] ? id[k] : 0) * width, column, width);
+#pragma unroll
+        for (int k = 0; k < kDots; k++)
+#pragma unroll
+            for (int e = 0; e < Slice<T>::V; e++) dot[k] = __builtin_fmaf(a.v[e], b[k].v[e], dot[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kDots; k++) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) dot[k] += __shfl_xor(dot[k], d, 64);
+        if (from + k < count) out(from + k, id[k], inside[k], dot[k]);
+    }
+}
+
 // The same for few tokens, where reading W is all that takes time, and for few logits: a block per 16 tokens and kFewColumns rows of W, whose four waves each sum a
 // quarter of the width.  W goes from memory to the registers of the one wave that uses it, a unit of 128 bytes per row ahead of the products,
 // so there are no barriers on the way and every wave has its own loads in flight; tokens are read from the caches, at half of W's bytes.
@@ -460,7 +515,7 @@ constexpr int kFewWaves = 4;
 template <typename T, typename S>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, const T *__restrict__ hidden, const T *__restrict__ weight,
                                                                int64_t width, uint32_t groups, int64_t parts, float2 *__restrict__ stats,
-                                                               float *__restrict__ picked, S softmax)
+                                                               float *__restrict__ picked, S softmax, typename S::Picks picks)
 {
     using E = Element<T>;
     using Frag = typename E::Frag;
@@ -468,8 +523,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
     constexpr int TN = kFewColumns / 16, kUnit = kStepBytes / int(sizeof(T)), kPitch = kFewColumns + 4;
     __shared__ __align__(16) float part[kFewWaves][16][kPitch];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t block = blockIdx.x / groups;
-    const int64_t n0 = int64_t(block) * kFewColumns, m0 = int64_t(blockIdx.x % groups) * kFewTokens;
+    uint32_t at_block = blockIdx.x;
+    if constexpr (!S::kTargets) {
+        if (at_block < picks.blocks) {                   // (their products take a few dependent loads, so they go ahead of W)
+            const int64_t item = int64_t(at_block) * kFewWaves + wave, each = (picks.count + kDots - 1) / kDots, token = item / each;
+            if (token >= tokens.tokens) return;
+            float *const out = picks.picked + token * picks.count;
+            entry_dots(hidden + token * width, weight, width, tokens.vocab, picks.ids + token * picks.count, picks.ignore, int(item % each) * kDots,
+                       picks.count, lane, [&](int k, int64_t, bool, float z) { if (lane == 0) out[k] = z; });
+            return;
+        }
+        at_block -= picks.blocks;
+    }
+    const uint32_t block = at_block / groups;
+    const int64_t n0 = int64_t(block) * kFewColumns, m0 = int64_t(at_block % groups) * kFewTokens;
     const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens - m0);
     // (rows past the last one are read from it, and not used)
     uint32_t of_column[TN];
@@ -1008,9 +1075,11 @@ struct Calls {
     void loss_of_few() const
     {
         const uint32_t groups = uint32_t((l.tokens + kFewTokens - 1) / kFewTokens);
-        few_tiles<T, S><<<dim3(uint32_t((l.vocab + kFewColumns - 1) / kFewColumns) * groups), 64 * kFewWaves, 0, stream>>>(
+        uint32_t more = 0;
+        if constexpr (!S::kTargets) more = picks.blocks;
+        few_tiles<T, S><<<dim3(uint32_t((l.vocab + kFewColumns - 1) / kFewColumns) * groups + more), 64 * kFewWaves, 0, stream>>>(
             tokens(), static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.width, groups, l.parts, at<float2>(l.stats),
-            at<float>(l.picked), softmax);
+            at<float>(l.picked), softmax, picks);
         launched();
     }
     template <int WAVES>
