@@ -86,7 +86,7 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortEach = 8
 
 struct SortShared {
     uint32_t place[kSortWaves][kDigits];     // entries of a digit in a wave's part, then where the next one of them goes
-    uint32_t waves[kSortWaves], all[kSortWaves];
+    uint32_t waves[kDigits / 64], ahead[kSortWaves], all;
 };
 
 __device__ __forceinline__ uint32_t wave_sum(uint32_t v)
@@ -96,31 +96,40 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t v)
     return v;
 }
 
-// One stable pass of a sort by digits, by a block: `read(i, key, token)` says whether entry i of n takes part, and `write(place, key, token)`
-// gets the entries in the order of the digit `key >> shift`, those of one digit in the order of i.  `counted(first)` is called by all threads
-// between the two walks over the entries.  Each wave takes a run of neighbouring entries, so that ranks within a digit follow from
+// One stable pass of a sort by digits, by a block: `read(load(i), i, exists, key, token)` says whether entry i of n takes part, and `write(place, key, token)`
+// gets the entries in the order of the digit `key >> shift`, those of one digit in the order of i.  `counted(n)` is called by all threads
+// between the two walks over the entries; thread 0's argument is how many take part.  Each wave takes a run of neighbouring entries, so that ranks within a digit follow from
 // the counts of the waves before it and, among its own 64 at a time, from votes.
-template <class Read, class Counted, class Write>
-__device__ __forceinline__ void sort_pass(SortShared &s, int64_t n, int shift, int bits, Read read, Counted counted, Write write)
+template <class Load, class Read, class Counted, class Write>
+__device__ __forceinline__ void sort_pass(SortShared &s, uint32_t n, int shift, int bits, Load load, Read read, Counted counted, Write write)
 {
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, from = wave * each, to = from + each < n ? from + each : n;
+    const uint32_t each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, from = uint32_t(wave) * each, to = from + each < n ? from + each : n;
     const uint32_t mask = (1u << bits) - 1;
-    for (int k = tid; k < kSortWaves * kDigits; k += kSortThreads) s.place[0][k] = 0;
+    // (all loads first, of entries that exist: none waits for another one's condition)
+    using Entry = decltype(load(0u));
+    const auto load_all = [&](uint32_t i, Entry (&entry)[kSortEach]) {
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++) {
+            const uint32_t at = i + 64 * k + lane;
+            entry[k] = load(at < to ? at : to - 1);
+        }
+    };
+    for (int k = tid; k < kSortWaves * kDigits; k += kSortThreads) s.place[k / kDigits][k % kDigits] = 0;
     __syncthreads();
-    for (int64_t i = from; i < to; i += 64 * kSortEach) {
-        uint32_t key[kSortEach] = {};
-        int32_t token[kSortEach] = {};
-        bool in[kSortEach];
+    for (uint32_t i = from; i < to; i += 64 * kSortEach) {
+        Entry entry[kSortEach];
+        load_all(i, entry);
 #pragma unroll
-        for (int k = 0; k < kSortEach; k++) in[k] = i + 64 * k + lane < to && read(i + 64 * k + lane, key[k], token[k]);
-#pragma unroll
-        for (int k = 0; k < kSortEach; k++)
-            if (in[k]) atomicAdd(&s.place[wave][(key[k] >> shift) & mask], 1u);
+        for (int k = 0; k < kSortEach; k++) {
+            uint32_t key;
+            int32_t token;
+            if (read(entry[k], i + 64 * k + lane, i + 64 * k + lane < to, key, token)) atomicAdd(&s.place[wave][(key >> shift) & mask], 1u);
+        }
     }
     __syncthreads();
     // places: digits in order, the waves of a digit in order
-    uint32_t mine = 0, before = 0;
+    uint32_t mine = 0, before = 0, sum = 0;
     if (tid < kDigits) {
         for (int w = 0; w < kSortWaves; w++) mine += s.place[w][tid];
         before = mine;
@@ -132,6 +141,7 @@ __device__ __forceinline__ void sort_pass(SortShared &s, int64_t n, int shift, i
         if (lane == 63) s.waves[wave] = before;
     }
     __syncthreads();
+    for (int w = 0; w < kDigits / 64; w++) sum += s.waves[w];
     if (tid < kDigits) {
         before -= mine;
         for (int w = 0; w < wave; w++) before += s.waves[w];
@@ -141,27 +151,27 @@ __device__ __forceinline__ void sort_pass(SortShared &s, int64_t n, int shift, i
             before += here;
         }
     }
-    counted();
+    counted(sum);
     __syncthreads();
-    for (int64_t i = from; i < to; i += 64 * kSortEach) {
-        uint32_t key[kSortEach] = {};
-        int32_t token[kSortEach] = {};
-        bool in[kSortEach];
-#pragma unroll
-        for (int k = 0; k < kSortEach; k++) in[k] = i + 64 * k + lane < to && read(i + 64 * k + lane, key[k], token[k]);
+    for (uint32_t i = from; i < to; i += 64 * kSortEach) {
+        Entry entry[kSortEach];
+        load_all(i, entry);
 #pragma unroll
         for (int k = 0; k < kSortEach; k++) {
-            const uint64_t vote = __ballot(in[k]);
+            uint32_t key;
+            int32_t token;
+            const bool in = read(entry[k], i + 64 * k + lane, i + 64 * k + lane < to, key, token);
+            const uint64_t vote = __ballot(in);
             if (!vote) continue;
-            const uint32_t digit = (key[k] >> shift) & mask;
+            const uint32_t digit = (key >> shift) & mask;
             uint64_t same = vote;
             for (int b = 0; b < bits; b++) {
                 const uint64_t ones = __ballot((digit >> b) & 1);
                 same &= (digit >> b) & 1 ? ones : ~ones;
             }
-            if (in[k]) {
+            if (in) {
                 const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1))), first = s.place[wave][digit];
-                write(first + rank, key[k], token[k]);
+                write(first + rank, key, token);
                 __builtin_amdgcn_wave_barrier();
                 if (rank == 0) s.place[wave][digit] = first + uint32_t(__popcll(same));
                 __builtin_amdgcn_wave_barrier();
@@ -200,52 +210,56 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__res
     __shared__ SortShared s;
     const int64_t low = int64_t(blockIdx.x) * share, high = low + share < vocab ? low + share : vocab;
     const int passes = bits <= kDigitBits ? 1 : (bits + kDigitBits - 1) / kDigitBits;
-    uint32_t ahead = 0, own = 0, base = 0, mine = 0;
+    uint32_t ahead = 0, base = 0, mine = 0;
     bool counting = true;
-    const auto from_ids = [&](int64_t i, uint32_t &key, int32_t &token) {
-        const int64_t id = ids[i];
-        const bool valid = id >= 0 && id < vocab && id != ignore, in = valid && id >= low && id < high;
-        if (counting) {
-            ahead += valid && id < low;
-            own += in;
+    // (every block does this for every token: few instructions.  As unsigned numbers, ids below 0 are above all others.)
+    const uint64_t from = uint64_t(low), span = uint64_t(high - low);
+    const bool marked = ignore >= 0 && ignore < vocab;
+    // (offsets of 32 bits from a uniform address: fewer than 2^24 tokens)
+    const auto load_id = [&](uint32_t i) { return *reinterpret_cast<const uint64_t *>(reinterpret_cast<const unsigned char *>(ids) + i * 8u); };
+    const auto from_ids = [&](uint64_t id, uint32_t i, bool exists, uint32_t &key, int32_t &token) {
+        bool in = exists && id - from < span, under = exists && id < from;
+        if (marked) {
+            in = in && id != uint64_t(ignore);
+            under = under && id != uint64_t(ignore);
         }
-        key = uint32_t(id - low);
+        if (counting) ahead += under;
+        key = uint32_t(id) - uint32_t(from);
         token = int32_t(i);
         return in;
     };
-    const auto totals = [&] {
+    const auto totals = [&](uint32_t own) {
         counting = false;
-        const uint32_t x = wave_sum(ahead), y = wave_sum(own);
-        if ((tid & 63) == 0) {
-            s.waves[tid >> 6] = x;
-            s.all[tid >> 6] = y;
-        }
+        const uint32_t x = wave_sum(ahead);
+        if ((tid & 63) == 0) s.ahead[tid >> 6] = x;
+        if (tid == 0) s.all = own;
         __syncthreads();
-        for (int w = 0; w < kSortWaves; w++) {
-            base += s.waves[w];
-            mine += s.all[w];
-        }
+        for (int w = 0; w < kSortWaves; w++) base += s.ahead[w];
+        mine = s.all;
         if (blockIdx.x == sort_blocks - 1 && tid == 0) header->count = int32_t(base + mine);
     };
     int to = (passes - 1) & 1;
     const auto put = [&](uint32_t place, uint32_t key, int32_t token) {
+        if (int64_t(base) + place >= tokens) return;     // (ids that change between the two walks, on another stream, write nothing outside)
         a.token[to][base + place] = token;
         a.id[to][base + place] = int32_t(low + key);
     };
     const int first_bits = bits < kDigitBits ? bits : kDigitBits;
-    // (sort_pass has read s.waves before it calls this, but not all waves may be done with it)
-    sort_pass(s, tokens, 0, first_bits, from_ids, [&] { __syncthreads(); totals(); }, put);
+    sort_pass(s, uint32_t(tokens), 0, first_bits, load_id, from_ids, totals, put);
     for (int p = 1; p < passes; p++) {
-        const int from = to;
+        const int32_t *token = a.token[to] + base, *id = a.id[to] + base;
         to ^= 1;
-        const int32_t *token = a.token[from] + base, *id = a.id[from] + base;
-        const auto from_list = [&](int64_t i, uint32_t &key, int32_t &t) {
-            key = uint32_t(id[i] - low);
-            t = token[i];
-            return true;
+        struct Held {
+            int32_t token, id;
+        };
+        const auto load_held = [&](uint32_t i) { return Held{token[i], id[i]}; };
+        const auto from_list = [&](Held e, uint32_t, bool exists, uint32_t &key, int32_t &t) {
+            key = uint32_t(e.id - int32_t(low));
+            t = e.token;
+            return exists;
         };
         const int left = bits - p * kDigitBits;
-        sort_pass(s, int64_t(mine), p * kDigitBits, left < kDigitBits ? left : kDigitBits, from_list, [] {}, put);
+        sort_pass(s, mine, p * kDigitBits, left < kDigitBits ? left : kDigitBits, load_held, from_list, [](uint32_t) {}, put);
     }
 }
 
@@ -347,7 +361,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *
     int64_t last = at + 1, end = (count + chunk - 1) / chunk;
     while (end - last > 1) {
         const int64_t step = (end - last + 63) / 64, guess = last + lane * step;
-        const int same = __popcll(__ballot(guess < end && ids[(guess < end ? guess : last) * chunk] == id));
+        const int found_here = __popcll(__ballot(guess < end && ids[(guess < end ? guess : last) * chunk] == id)), same = found_here > 0 ? found_here : 1;
         const int64_t found = last + int64_t(same - 1) * step;
         end = found + step < end ? found + step : end;
         last = found;
@@ -368,7 +382,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *
 #pragma unroll
     for (int e = 0; e < P::V; e++) acc[e] = 0.f;
     if (wave == 0) add(partial + (at * 2 + 1) * pitch + column);
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t c = at + 1 + wave * each; c < to; c++) add(partial + c * 2 * pitch + column);
     put_partial(&sums[wave][lane * P::V], acc);
     __syncthreads();
@@ -377,6 +391,64 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *
     for (int e = 0; e < P::V; e++) acc[e] = 0.f;
     for (int w = 0; w < kJoinWaves; w++) add(&sums[w][lane * P::V]);
     finish<T>(acc, scale, accumulate != 0, dtable + int64_t(id) * width, column, width);
+}
+
+// Few tokens: no sort.  Every wave holds all ids, two a lane, and finds the tokens of a row by votes.  A wave takes a strip of kFewRows rows of the table,
+// one after another, or (accumulate) that of one token's row, if it is the first token of its id.
+constexpr int kFewTokens = 128, kFewRows = 4;
+template <typename T>
+__global__ __launch_bounds__(kBlock) void few_rows(const int64_t *__restrict__ ids, const T *__restrict__ dout, int32_t tokens, int64_t ignore,
+                                                   int64_t vocab, int64_t width, uint32_t strips, float scale, int32_t accumulate,
+                                                   T *__restrict__ dtable)
+{
+    using P = Piece<T>;
+    const int lane = int(threadIdx.x) & 63;
+    const int64_t item = int64_t(blockIdx.x) * (kBlock / 64) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), at = item / strips;
+    const int64_t column = (item % strips * 64 + lane) * P::V;
+    const auto id_of = [&](int32_t token) {
+        const int64_t id = token < tokens ? ids[token] : -1;
+        return id >= 0 && id < vocab && id != ignore ? int32_t(id) : -1;
+    };
+    const int32_t low = id_of(lane), high = id_of(64 + lane);
+    const auto sum = [&](uint64_t first, uint64_t second, int32_t id) {
+        float acc[P::V];
+#pragma unroll
+        for (int e = 0; e < P::V; e++) acc[e] = 0.f;
+        while (first | second) {
+            typename P::Vec v[kAhead];
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                v[k] = typename P::Vec(T(0.f));
+                if (!(first | second)) continue;
+                const int64_t token = first ? __builtin_ctzll(first) : 64 + __builtin_ctzll(second);
+                if (first) first &= first - 1;
+                else second &= second - 1;
+                if (column < width) v[k] = P::load(dout + token * width, column, width);
+                n = k + 1;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                if (k >= n) break;
+#pragma unroll
+                for (int e = 0; e < P::V; e++) acc[e] += float(v[k][e]);
+            }
+        }
+        if (column < width) finish<T>(acc, scale, accumulate != 0, dtable + int64_t(id) * width, column, width);
+    };
+    if (accumulate) {
+        if (at >= tokens) return;
+        const int32_t id = at < 64 ? __builtin_amdgcn_readlane(low, int(at)) : __builtin_amdgcn_readlane(high, int(at) - 64);
+        const uint64_t first = __ballot(low == id), second = __ballot(high == id);
+        if (id < 0 || (at < 64 ? first & ((uint64_t(1) << at) - 1) : first | (second & ((uint64_t(1) << (at - 64)) - 1)))) return;
+        sum(first, second, id);
+        return;
+    }
+    for (int64_t row = at * kFewRows; row < (at + 1) * kFewRows && row < vocab; row++) {
+        const uint64_t first = __ballot(low == int32_t(row)), second = __ballot(high == int32_t(row));
+        if (first | second) sum(first, second, int32_t(row));
+        else if (column < width) P::store(dtable + row * width, column, width, typename P::Vec(T(0.f)));
+    }
 }
 
 // ---------------------------------------------------------------- launches
@@ -415,6 +487,14 @@ hipError_t gradient(const EmbedLayout &l, const void *dout, const int64_t *ids, 
                     unsigned char *ws, hipStream_t stream)
 {
     Launches g{stream};
+    if (l.tokens && l.tokens <= kFewTokens) {
+        const int64_t items = (accumulate ? l.tokens : (l.vocab + kFewRows - 1) / kFewRows) * l.strips;
+        few_rows<T><<<dim3(uint32_t((items + kBlock / 64 - 1) / (kBlock / 64))), kBlock, 0, stream>>>(
+            ids, static_cast<const T *>(dout), int32_t(l.tokens), ignore, l.vocab, l.width, uint32_t(l.strips), scale, accumulate,
+            static_cast<T *>(dtable));
+        g.launched();
+        return g.error;
+    }
     const auto at = [ws](size_t offset) { return reinterpret_cast<int32_t *>(ws + offset); };
     EmbedHeader *header = reinterpret_cast<EmbedHeader *>(ws);
     const SortArrays a{{at(l.token[0]), at(l.token[1])}, {at(l.id[0]), at(l.id[1])}};
