@@ -15,6 +15,12 @@ int embed_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, EmbedLayo
     l.vocab = vocab;
     l.dt = dt;
     l.share = (vocab + kEmbedSortBlocks - 1) / kEmbedSortBlocks;
+    l.parts = tokens > kEmbedManyTokens;
+    if (l.parts) {
+        int64_t share = 1;
+        while (share < l.share) share *= 2;
+        l.share = share;
+    }
     l.blocks = int32_t((vocab + l.share - 1) / l.share);
     while (int64_t(1) << l.bits < l.share) l.bits++;
     const int64_t columns = dt == CGX_F32 ? 256 : 512;
@@ -31,9 +37,10 @@ int embed_layout(int64_t tokens, int64_t width, int64_t vocab, int dt, EmbedLayo
         return here;
     };
     const int arrays = l.bits > 8 ? 2 : 1;
-    for (int k = 0; k < arrays; k++) {
-        l.token[k] = take(tokens * 4);
-        l.id[k] = take(tokens * 4);
+    for (int k = 0; k < arrays; k++) l.list[k] = take(tokens * int64_t(sizeof(SortedToken)));
+    if (l.parts) {
+        l.part = take(tokens * int64_t(sizeof(SortedToken)));
+        l.starts = take((l.blocks + 1) * kEmbedParts * 4);
     }
     l.partial = take(l.chunks * 2 * l.pitch * 4);
     l.bytes = at;

@@ -96,37 +96,53 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t v)
     return v;
 }
 
-// One stable pass of a sort by digits, by a block: `read(load(i), i, exists, key, token)` says whether entry i of n takes part, and `write(place, key, token)`
-// gets the entries in the order of the digit `key >> shift`, those of one digit in the order of i.  `counted(n)` is called by all threads
-// between the two walks over the entries; thread 0's argument is how many take part.  Each wave takes a run of neighbouring entries, so that ranks within a digit follow from
-// the counts of the waves before it and, among its own 64 at a time, from votes.
-template <class Load, class Read, class Counted, class Write>
-__device__ __forceinline__ void sort_pass(SortShared &s, uint32_t n, int shift, int bits, Load load, Read read, Counted counted, Write write)
+// A wave's walk over entries `from` to `to` of a list, 64 at a time: `visit(entry, i, exists)`, called by all lanes.  All loads first, of entries that
+// exist: none waits for another one's condition.
+template <class Load, class Visit>
+__device__ __forceinline__ void walk(uint32_t from, uint32_t to, int lane, Load load, Visit visit)
 {
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, from = uint32_t(wave) * each, to = from + each < n ? from + each : n;
-    const uint32_t mask = (1u << bits) - 1;
-    // (all loads first, of entries that exist: none waits for another one's condition)
-    using Entry = decltype(load(0u));
-    const auto load_all = [&](uint32_t i, Entry (&entry)[kSortEach]) {
+    for (uint32_t i = from; i < to; i += 64 * kSortEach) {
+        decltype(load(0u)) entry[kSortEach];
 #pragma unroll
         for (int k = 0; k < kSortEach; k++) {
             const uint32_t at = i + 64 * k + lane;
             entry[k] = load(at < to ? at : to - 1);
         }
-    };
+#pragma unroll
+        for (int k = 0; k < kSortEach; k++) visit(entry[k], i + 64 * k + lane, i + 64 * k + lane < to);
+    }
+}
+// The walk of a wave's share of n entries: a run of neighbouring ones.
+template <class Load>
+struct Run {
+    uint32_t from, to;
+    Load load;
+    __device__ __forceinline__ Run(uint32_t n, int wave, Load l) : load(l)
+    {
+        const uint32_t each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+        from = uint32_t(wave) * each;
+        to = from + each < n ? from + each : n;
+    }
+    template <class Visit>
+    __device__ __forceinline__ void operator()(int lane, Visit visit) const { walk(from, to, lane, load, visit); }
+};
+
+// One stable pass of a sort by digits, by a block.  `run(lane, visit)` walks over a wave's entries, those of the waves one after another; `read(entry, i,
+// exists, key, token)` says whether an entry takes part, and `write(place, key, token)` gets the entries in the order of the digit `key >> shift`, those of
+// one digit in the order they come in.  `counted(n)` is called by all threads between the two walks; thread 0's argument is how many take part.  Ranks
+// within a digit follow from the counts of the waves before and, among a wave's own 64 at a time, from votes.
+template <class Walk, class Read, class Counted, class Write>
+__device__ __forceinline__ void sort_pass(SortShared &s, int shift, int bits, Walk run, Read read, Counted counted, Write write)
+{
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t mask = (1u << bits) - 1;
     for (int k = tid; k < kSortWaves * kDigits; k += kSortThreads) s.place[k / kDigits][k % kDigits] = 0;
     __syncthreads();
-    for (uint32_t i = from; i < to; i += 64 * kSortEach) {
-        Entry entry[kSortEach];
-        load_all(i, entry);
-#pragma unroll
-        for (int k = 0; k < kSortEach; k++) {
-            uint32_t key;
-            int32_t token;
-            if (read(entry[k], i + 64 * k + lane, i + 64 * k + lane < to, key, token)) atomicAdd(&s.place[wave][(key >> shift) & mask], 1u);
-        }
-    }
+    run(lane, [&](auto entry, uint32_t i, bool exists) {
+        uint32_t key;
+        int32_t token;
+        if (read(entry, i, exists, key, token)) atomicAdd(&s.place[wave][(key >> shift) & mask], 1u);
+    });
     __syncthreads();
     // places: digits in order, the waves of a digit in order
     uint32_t mine = 0, before = 0, sum = 0;
@@ -153,48 +169,97 @@ __device__ __forceinline__ void sort_pass(SortShared &s, uint32_t n, int shift, 
     }
     counted(sum);
     __syncthreads();
-    for (uint32_t i = from; i < to; i += 64 * kSortEach) {
-        Entry entry[kSortEach];
-        load_all(i, entry);
-#pragma unroll
-        for (int k = 0; k < kSortEach; k++) {
-            uint32_t key;
-            int32_t token;
-            const bool in = read(entry[k], i + 64 * k + lane, i + 64 * k + lane < to, key, token);
-            const uint64_t vote = __ballot(in);
-            if (!vote) continue;
-            const uint32_t digit = (key >> shift) & mask;
-            uint64_t same = vote;
-            for (int b = 0; b < bits; b++) {
-                const uint64_t ones = __ballot((digit >> b) & 1);
-                same &= (digit >> b) & 1 ? ones : ~ones;
-            }
-            if (in) {
-                const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1))), first = s.place[wave][digit];
-                write(first + rank, key, token);
-                __builtin_amdgcn_wave_barrier();
-                if (rank == 0) s.place[wave][digit] = first + uint32_t(__popcll(same));
-                __builtin_amdgcn_wave_barrier();
-            }
+    run(lane, [&](auto entry, uint32_t i, bool exists) {
+        uint32_t key;
+        int32_t token;
+        const bool in = read(entry, i, exists, key, token);
+        const uint64_t vote = __ballot(in);
+        if (!vote) return;
+        const uint32_t digit = (key >> shift) & mask;
+        uint64_t same = vote;
+        for (int b = 0; b < bits; b++) {
+            const uint64_t ones = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? ones : ~ones;
         }
-    }
+        if (in) {
+            const uint32_t rank = __builtin_amdgcn_mbcnt_hi(uint32_t(same >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(same), 0u));
+            const uint32_t first = s.place[wave][digit];
+            write(first + rank, key, token);
+            __builtin_amdgcn_wave_barrier();
+            if (rank == 0) s.place[wave][digit] = first + uint32_t(__popcll(same));
+            __builtin_amdgcn_wave_barrier();
+        }
+    });
     __syncthreads();
 }
 
-struct SortArrays {
-    int32_t *token[2], *id[2];
+// Lists are read and written with offsets of 32 bits from a uniform address: they have fewer than 2^24 entries.
+template <typename U>
+__device__ __forceinline__ U &listed(U *list, uint32_t at)
+{
+    using Bytes = std::conditional_t<std::is_const<U>::value, const unsigned char, unsigned char>;
+    return *reinterpret_cast<U *>(reinterpret_cast<Bytes *>(list) + at * uint32_t(sizeof(U)));
+}
+
+// Ids of a share [from, from + span) of the vocabulary.  Few instructions: every block does this for every token.
+struct Id {
+    uint32_t low, high;
+};
+struct Share {
+    uint32_t from, span, mark;
+    bool marked;             // `ignore` is an entry of the vocabulary
+    __device__ __forceinline__ Share(int64_t low, int64_t high, int64_t vocab, int64_t ignore)
+        : from(uint32_t(low)), span(uint32_t(high - low)), mark(uint32_t(ignore)), marked(ignore >= 0 && ignore < vocab) {}
+    __device__ __forceinline__ bool valid(Id id) const { return id.high == 0 && !(marked && id.low == mark); }       // (or beyond the vocabulary)
+    __device__ __forceinline__ uint32_t key(Id id) const { return id.low - from; }
+    __device__ __forceinline__ bool has(Id id) const { return valid(id) && key(id) < span; }
 };
 
-// The first sort_blocks blocks sort: each looks at all ids for those of its share of the vocabulary, and for how many there are ahead of it, and
-// sorts its own, stably, eight bits of their place in the share at a time (one pass for up to 65536 entries).  The blocks behind them write
-// zeros over the table meanwhile, which hides the sort wherever the table is long.
-constexpr int kFillBytes = 64 << 10;                 // of the table, a block
-template <bool FILL>
-__global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__restrict__ ids, int64_t tokens, int64_t ignore, int64_t vocab,
-                                                            int64_t share, int32_t bits, uint32_t sort_blocks, EmbedHeader *header,
-                                                            SortArrays a, unsigned char *__restrict__ table, int64_t bytes)
+// Many tokens: first, blocks sort a part of them each by share.  starts[share][part]: where a share begins in a part.
+struct Parts {
+    SortedToken *list;
+    uint32_t *starts;
+    uint32_t each;           // tokens of a part
+    int32_t share_bits;
+};
+__global__ __launch_bounds__(kSortThreads) void sort_parts(const int64_t *__restrict__ ids, uint32_t tokens, int64_t ignore, int64_t vocab, int32_t shares, Parts parts)
 {
-    const int tid = int(threadIdx.x);
+    __shared__ SortShared s;
+    const int tid = int(threadIdx.x), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t first = blockIdx.x * parts.each < tokens ? blockIdx.x * parts.each : tokens, n = tokens - first < parts.each ? tokens - first : parts.each;
+    const Share all(0, vocab, vocab, ignore);
+    const Id *const own = reinterpret_cast<const Id *>(ids) + first;
+    sort_pass(
+        s, parts.share_bits, kDigitBits, Run(n, wave, [&](uint32_t i) { return listed(own, i); }),
+        [&](Id id, uint32_t i, bool exists, uint32_t &key, int32_t &token) {
+            key = id.low;
+            token = int32_t(first + i);
+            return exists && all.has(id);
+        },
+        [&](uint32_t count) {
+            // (a digit's places have been written by this thread)
+            if (tid < shares && tid < kDigits) parts.starts[tid * kEmbedParts + blockIdx.x] = s.place[0][tid];
+            if (tid == 0) parts.starts[shares * kEmbedParts + blockIdx.x] = count;
+        },
+        [&](uint32_t place, uint32_t key, int32_t token) {
+            if (place < n) listed(parts.list + first, place) = SortedToken{int32_t(key), token};
+        });
+}
+
+// The first sort_blocks blocks sort the tokens of a share of the vocabulary each, stably, eight bits of their place in the share at a time (one pass for up
+// to 65536 entries).  Up to some thousand tokens a block finds its own by looking at all ids, and learns from them how many there are ahead of it
+// (PARTS false); these 256 looks at every token cost more than a launch from kEmbedManyTokens on, where it takes its share from every part instead.
+// The blocks behind them write zeros over the table meanwhile, which hides the sort wherever the table is long.
+// 65536 tokens of 259 entries: 36 us looking at all ids, whether 8 or 16 loads of a lane are on their way, and with half the instructions: 128 visits of 64
+// ids by each of a block's waves.
+constexpr int kFillBytes = 64 << 10;                 // of the table, a block
+template <bool FILL, bool PARTS>
+__global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__restrict__ ids, uint32_t tokens, int64_t ignore, int64_t vocab,
+                                                            int64_t share, int32_t bits, uint32_t sort_blocks, EmbedHeader *header,
+                                                            SortedToken *list, SortedToken *between, Parts parts,
+                                                            unsigned char *__restrict__ table, int64_t bytes)
+{
+    const int tid = int(threadIdx.x), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (FILL && blockIdx.x >= sort_blocks) {
         typedef uint32_t Vec __attribute__((ext_vector_type(4)));
         const int64_t first = int64_t(blockIdx.x - sort_blocks) * kFillBytes;
@@ -209,57 +274,86 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__res
     }
     __shared__ SortShared s;
     const int64_t low = int64_t(blockIdx.x) * share, high = low + share < vocab ? low + share : vocab;
-    const int passes = bits <= kDigitBits ? 1 : (bits + kDigitBits - 1) / kDigitBits;
-    uint32_t ahead = 0, base = 0, mine = 0;
-    bool counting = true;
-    // (every block does this for every token: few instructions.  As unsigned numbers, ids below 0 are above all others.)
-    const uint64_t from = uint64_t(low), span = uint64_t(high - low);
-    const bool marked = ignore >= 0 && ignore < vocab;
-    // (offsets of 32 bits from a uniform address: fewer than 2^24 tokens)
-    const auto load_id = [&](uint32_t i) { return *reinterpret_cast<const uint64_t *>(reinterpret_cast<const unsigned char *>(ids) + i * 8u); };
-    const auto from_ids = [&](uint64_t id, uint32_t i, bool exists, uint32_t &key, int32_t &token) {
-        bool in = exists && id - from < span, under = exists && id < from;
-        if (marked) {
-            in = in && id != uint64_t(ignore);
-            under = under && id != uint64_t(ignore);
-        }
-        if (counting) ahead += under;
-        key = uint32_t(id) - uint32_t(from);
-        token = int32_t(i);
-        return in;
+    const Share own(low, high, vocab, ignore);
+    const int passes = bits <= kDigitBits ? 1 : (bits + kDigitBits - 1) / kDigitBits, first_bits = bits < kDigitBits ? bits : kDigitBits;
+    uint32_t base = 0, mine = 0;
+    SortedToken *to = passes % 2 ? list : between;
+    const auto put = [&](uint32_t place, uint32_t key, int32_t token) {
+        const uint32_t at = base + place;
+        if (at < tokens) listed(to, at) = SortedToken{int32_t(own.from + key), token};       // (even if ids change between two walks over them)
     };
-    const auto totals = [&](uint32_t own) {
-        counting = false;
+    const auto from_list = [&](SortedToken e, uint32_t, bool exists, uint32_t &key, int32_t &token) {
+        key = uint32_t(e.id) - own.from;
+        token = e.token;
+        return exists;
+    };
+    // A sum over the block, in every thread; `own` is thread 0's.
+    const auto totals = [&](uint32_t ahead, uint32_t count) {
         const uint32_t x = wave_sum(ahead);
         if ((tid & 63) == 0) s.ahead[tid >> 6] = x;
-        if (tid == 0) s.all = own;
+        if (tid == 0) s.all = count;
         __syncthreads();
         for (int w = 0; w < kSortWaves; w++) base += s.ahead[w];
         mine = s.all;
         if (blockIdx.x == sort_blocks - 1 && tid == 0) header->count = int32_t(base + mine);
     };
-    int to = (passes - 1) & 1;
-    const auto put = [&](uint32_t place, uint32_t key, int32_t token) {
-        if (int64_t(base) + place >= tokens) return;     // (ids that change between the two walks, on another stream, write nothing outside)
-        a.token[to][base + place] = token;
-        a.id[to][base + place] = int32_t(low + key);
-    };
-    const int first_bits = bits < kDigitBits ? bits : kDigitBits;
-    sort_pass(s, uint32_t(tokens), 0, first_bits, load_id, from_ids, totals, put);
+    if constexpr (PARTS) {
+        __shared__ uint32_t start[kEmbedParts], length[kEmbedParts];
+        uint32_t from = 0, n = 0;
+        if (tid < kEmbedParts) {
+            from = parts.starts[blockIdx.x * kEmbedParts + tid];
+            n = parts.starts[(blockIdx.x + 1) * kEmbedParts + tid] - from;
+            start[tid] = uint32_t(tid) * parts.each + from;
+            length[tid] = n;
+        }
+        const uint32_t count = wave_sum(n);
+        if ((tid & 63) == 0 && tid < kEmbedParts) s.waves[tid >> 6] = count;
+        __syncthreads();
+        uint32_t all = 0;
+        for (int w = 0; w < kEmbedParts / 64; w++) all += s.waves[w];
+        totals(from, all);                               // (what is ahead of this share in every part)
+        // Neighbouring parts a wave: what several of them begin with, up to 64 each, is on its way at a time.
+        const auto load = [&](uint32_t at) { return listed(parts.list, at < tokens ? at : 0u); };
+        const auto run = [&](int lane, auto visit) {
+            constexpr int kEach = kEmbedParts / kSortWaves;
+            for (int p0 = wave * kEach; p0 < (wave + 1) * kEach; p0 += kSortEach) {
+                SortedToken entry[kSortEach];
+#pragma unroll
+                for (int k = 0; k < kSortEach; k++) entry[k] = load(start[p0 + k] + (uint32_t(lane) < length[p0 + k] ? lane : 0));
+#pragma unroll
+                for (int k = 0; k < kSortEach; k++) {
+                    const uint32_t first = start[p0 + k], here = __builtin_amdgcn_readfirstlane(length[p0 + k]);
+                    visit(entry[k], 0u, uint32_t(lane) < here);
+                    if (here > 64) walk(64, here, lane, [&](uint32_t i) { return load(first + i); }, visit);
+                }
+            }
+        };
+        sort_pass(s, 0, first_bits, run, from_list, [](uint32_t) {}, put);
+    } else {
+        uint32_t ahead = 0;
+        bool counting = true;
+        const Id *const all = reinterpret_cast<const Id *>(ids);
+        const auto from_ids = [&](Id id, uint32_t i, bool exists, uint32_t &key, int32_t &token) {
+            const bool valid = exists && own.valid(id);
+            if (counting) ahead += valid && id.low < own.from;
+            key = own.key(id);
+            token = int32_t(i);
+            return valid && key < own.span;
+        };
+        sort_pass(
+            s, 0, first_bits, Run(tokens, wave, [&](uint32_t i) { return listed(all, i); }), from_ids,
+            [&](uint32_t count) {
+                counting = false;
+                totals(ahead, count);
+            },
+            put);
+    }
     for (int p = 1; p < passes; p++) {
-        const int32_t *token = a.token[to] + base, *id = a.id[to] + base;
-        to ^= 1;
-        struct Held {
-            int32_t token, id;
-        };
-        const auto load_held = [&](uint32_t i) { return Held{token[i], id[i]}; };
-        const auto from_list = [&](Held e, uint32_t, bool exists, uint32_t &key, int32_t &t) {
-            key = uint32_t(e.id - int32_t(low));
-            t = e.token;
-            return exists;
-        };
+        SortedToken *const from = to + base;
+        to = to == list ? between : list;
         const int left = bits - p * kDigitBits;
-        sort_pass(s, mine, p * kDigitBits, left < kDigitBits ? left : kDigitBits, load_held, from_list, [](uint32_t) {}, put);
+        sort_pass(s, p * kDigitBits, left < kDigitBits ? left : kDigitBits, Run(mine, wave, [&](uint32_t i) { return listed(from, i); }), from_list,
+                  [](uint32_t) {}, put);
     }
 }
 
@@ -293,7 +387,7 @@ __device__ __forceinline__ void put_partial(float *p, const float (&acc)[V])
 // it began in is finished here; what a chunk has of a run that came from the chunk before, and of one that goes on in the next, is left for join_runs.
 constexpr int kAhead = 8;
 template <typename T>
-__global__ __launch_bounds__(kBlock) void sum_chunks(const EmbedHeader *header, const int32_t *__restrict__ tokens, const int32_t *__restrict__ ids,
+__global__ __launch_bounds__(kBlock) void sum_chunks(const EmbedHeader *header, const SortedToken *__restrict__ list,
                                                      const T *__restrict__ dout, int64_t width, uint32_t strips, int32_t chunk, float scale,
                                                      int32_t accumulate, T *__restrict__ dtable, float *__restrict__ partial, int64_t pitch)
 {
@@ -304,8 +398,9 @@ __global__ __launch_bounds__(kBlock) void sum_chunks(const EmbedHeader *header, 
     const int64_t count = header->count, p0 = int64_t(at) * chunk;
     if (p0 >= count) return;
     const int n = int(count - p0 < chunk ? count - p0 : chunk);
-    const int32_t mine = lane < n ? ids[p0 + lane] : -1, from = lane < n ? tokens[p0 + lane] : 0;
-    const int32_t before = p0 > 0 ? ids[p0 - 1] : -1, after = p0 + n < count ? ids[p0 + n] : -1;
+    const SortedToken held = lane < n ? list[p0 + lane] : SortedToken{-1, 0};
+    const int32_t mine = held.id, from = held.token;
+    const int32_t before = p0 > 0 ? list[p0 - 1].id : -1, after = p0 + n < count ? list[p0 + n].id : -1;
     const int64_t column = (int64_t(strip) * 64 + lane) * P::V;
     const bool there = column < width;
     float acc[P::V];
@@ -344,7 +439,7 @@ __global__ __launch_bounds__(kBlock) void sum_chunks(const EmbedHeader *header, 
 // chunks each.
 constexpr int kJoinWaves = 8;
 template <typename T>
-__global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *header, const int32_t *__restrict__ ids, int64_t width,
+__global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *header, const SortedToken *__restrict__ list, int64_t width,
                                                              uint32_t strips, int32_t chunk, float scale, int32_t accumulate,
                                                              T *__restrict__ dtable, const float *__restrict__ partial, int64_t pitch)
 {
@@ -355,13 +450,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_runs(const EmbedHeader *
     const int64_t at = blockIdx.x / strips, strip = blockIdx.x % strips;
     const int64_t count = header->count, p0 = at * chunk;
     if (p0 + chunk >= count) return;                     // nothing after this chunk
-    const int32_t id = ids[p0 + chunk - 1];
-    if (ids[p0 + chunk] != id || (p0 > 0 && ids[p0 - 1] == id)) return;
+    const int32_t id = list[p0 + chunk - 1].id;
+    if (list[p0 + chunk].id != id || (p0 > 0 && list[p0 - 1].id == id)) return;
     // the last chunk that begins with this id, 64 guesses at a time
     int64_t last = at + 1, end = (count + chunk - 1) / chunk;
     while (end - last > 1) {
         const int64_t step = (end - last + 63) / 64, guess = last + lane * step;
-        const int found_here = __popcll(__ballot(guess < end && ids[(guess < end ? guess : last) * chunk] == id)), same = found_here > 0 ? found_here : 1;
+        const int found_here = __popcll(__ballot(guess < end && list[(guess < end ? guess : last) * chunk].id == id)), same = found_here > 0 ? found_here : 1;
         const int64_t found = last + int64_t(same - 1) * step;
         end = found + step < end ? found + step : end;
         last = found;
@@ -495,29 +590,37 @@ hipError_t gradient(const EmbedLayout &l, const void *dout, const int64_t *ids, 
         g.launched();
         return g.error;
     }
-    const auto at = [ws](size_t offset) { return reinterpret_cast<int32_t *>(ws + offset); };
+    const auto at = [ws](size_t offset) { return reinterpret_cast<SortedToken *>(ws + offset); };
     EmbedHeader *header = reinterpret_cast<EmbedHeader *>(ws);
-    const SortArrays a{{at(l.token[0]), at(l.token[1])}, {at(l.id[0]), at(l.id[1])}};
+    SortedToken *const list = at(l.list[0]);
+    const Parts parts{at(l.part), reinterpret_cast<uint32_t *>(ws + l.starts), uint32_t((l.tokens + kEmbedParts - 1) / kEmbedParts), l.bits};
     const int64_t bytes = l.vocab * l.width * int64_t(sizeof(T)), fills = accumulate ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
     const uint32_t sorts = l.tokens ? uint32_t(l.blocks) : 0, grid = sorts + uint32_t(fills);
-    if (grid) {
-        if (fills)
-            sort_tokens<true><<<dim3(grid), kSortThreads, 0, stream>>>(ids, l.tokens, ignore, l.vocab, l.share, l.bits, sorts, header, a,
-                                                                       static_cast<unsigned char *>(dtable), bytes);
-        else
-            sort_tokens<false><<<dim3(grid), kSortThreads, 0, stream>>>(ids, l.tokens, ignore, l.vocab, l.share, l.bits, sorts, header, a, nullptr, 0);
+    if (l.parts) {
+        sort_parts<<<dim3(kEmbedParts), kSortThreads, 0, stream>>>(ids, uint32_t(l.tokens), ignore, l.vocab, l.blocks, parts);
         g.launched();
+    }
+    const auto sort = [&](auto fill, auto in_parts) {
+        sort_tokens<decltype(fill)::value, decltype(in_parts)::value><<<dim3(grid), kSortThreads, 0, stream>>>(
+            ids, uint32_t(l.tokens), ignore, l.vocab, l.share, l.bits, sorts, header, list, at(l.list[1]), parts, static_cast<unsigned char *>(dtable), bytes);
+        g.launched();
+    };
+    if (grid) {
+        const std::true_type yes;
+        const std::false_type no;
+        if (l.parts) fills ? sort(yes, yes) : sort(no, yes);
+        else fills ? sort(yes, no) : sort(no, no);
     }
     if (!l.tokens) return g.error;
     float *partial = reinterpret_cast<float *>(ws + l.partial);
     const int64_t items = l.chunks * l.strips;
     sum_chunks<T><<<dim3(uint32_t((items + kBlock / 64 - 1) / (kBlock / 64))), kBlock, 0, stream>>>(
-        header, a.token[0], a.id[0], static_cast<const T *>(dout), l.width, uint32_t(l.strips), l.chunk, scale, accumulate,
+        header, list, static_cast<const T *>(dout), l.width, uint32_t(l.strips), l.chunk, scale, accumulate,
         static_cast<T *>(dtable), partial, l.pitch);
     g.launched();
     if (l.chunks > 1) {
         join_runs<T><<<dim3(uint32_t((l.chunks - 1) * l.strips)), 64 * kJoinWaves, 0, stream>>>(
-            header, a.id[0], l.width, uint32_t(l.strips), l.chunk, scale, accumulate, static_cast<T *>(dtable), partial, l.pitch);
+            header, list, l.width, uint32_t(l.strips), l.chunk, scale, accumulate, static_cast<T *>(dtable), partial, l.pitch);
         g.launched();
     }
     return g.error;

@@ -313,3 +313,22 @@ def test_a_tied_table_gets_both_its_gradients(torch):
         # 2-norms; per element: hidden states, d, dhidden, dweight and their sum are rounded once each, every one by at most u of what it holds, and the
         # parts' norms are at most a few times the sum's
         assert off <= 5 * 4 * ROUNDOFF[dtype] + (1e-5 if dtype == "f32" else 0.0)
+
+
+@pytest.mark.parametrize("vocab", [3, 700, 66000, 1 << 20])
+def test_many_tokens_with_padding_and_ids_outside(torch, vocab):
+    """Longer lists of tokens are cut into parts before they are sorted."""
+    n, width = 40001, 40
+    dout = torch.randn(n, width).bfloat16().cuda()
+    ids = tokens_of(torch, n, vocab, "text", seed=3).cuda()
+    k = torch.arange(n, device="cuda")
+    ids[k % 11 == 3] = -100
+    ids[k % 13 == 5] = vocab
+    ids[k % 17 == 2] = (1 << 32) + 1
+    ids[5000:9000] = -100
+    dout[ids == -100] = float("nan")
+    gradient(torch, dout, ids, vocab)
+    gradient(torch, dout, ids, vocab, before=torch.randn(vocab, width).bfloat16().cuda())
+    dout[ids == -100] = 0.5
+    dout[ids == 1] = float("nan")
+    gradient(torch, dout, ids, vocab, ignore=1)                # an entry of the vocabulary as padding
