@@ -32,6 +32,14 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     if (grad) {
         at = shared;
         l.share = take(tokens * entries * 4);
+        l.lower = dt != CGX_F32 && tokens > 0 && tokens <= kLowerTokens;
+        l.other = dt == CGX_BF16 && tokens > kLowerTokens;
+        if (l.other) {
+            l.most = take(2 * kConvertBlocks * 4);
+            l.scales = take(2 * 4);
+            l.hidden16 = take(l.head.rows * l.head.pitch * 2);
+            l.weight16 = take(l.head.piece * l.head.pitch * 2);
+        }
         end = at > end ? at : end;
     }
     l.bytes = end;

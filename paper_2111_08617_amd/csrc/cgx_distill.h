@@ -18,8 +18,17 @@ struct DistillLayout {
     size_t entry = 0;        // Entry [tokens][entries]: sorted by id; those that are none are the last, with an id of -1
     size_t share = 0;        // float [tokens][entries] (gradient): of the entries in that order; ids that come again have theirs added to the first
     size_t strip = 0;        // uint16 [tokens][strips] (loss, tiles): see Picks
+    bool lower = false;      // (gradient) d is held in two parts, see Calls
+    bool other = false;      // (gradient) d, and the operands of its products, are held in binary16 instead of bfloat16
+    size_t most = 0;         // float [2][kConvertBlocks]: the largest magnitudes that the blocks of a conversion have seen
+    size_t scales = 0;       // float [2]: of the converted hidden states and of the weight's piece
+    size_t hidden16 = 0;     // binary16 [rows][pitch]
+    size_t weight16 = 0;     // binary16 [piece][pitch]
     size_t bytes = 0;
 };
+
+constexpr int kConvertBlocks = 1024;
+constexpr int64_t kLowerTokens = 128;                // up to this many tokens take d in two parts: rows for both are there
 
 // CGX_OK and the layout, or the error of the sizes.
 int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries, int dt, bool grad, DistillLayout *out);

@@ -239,11 +239,11 @@ __global__ __launch_bounds__(64 * kGatherWaves) void join_gathered(Teacher teach
 }
 
 // d at the teacher's entries within a piece of the vocabulary, in its units: a thread per entry.
-template <typename T>
-__global__ __launch_bounds__(256) void delta_entries(const Entry *__restrict__ entries, const float *__restrict__ shares, int32_t count, int64_t all,
-                                                     const int32_t *__restrict__ place, const float *__restrict__ lse,
+template <typename T, typename D, bool LOWER>
+__global__ __launch_bounds__(256) void delta_entries(const Header *header, const Entry *__restrict__ entries, const float *__restrict__ shares,
+                                                     int32_t count, int64_t all, const int32_t *__restrict__ place, const float *__restrict__ lse,
                                                      const float *__restrict__ factor, const float *__restrict__ picked, float inverse, int64_t from,
-                                                     int64_t columns, T *__restrict__ delta, int64_t piece)
+                                                     int64_t columns, D *__restrict__ delta, int64_t piece)
 {
     const int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (k >= all) return;
@@ -254,7 +254,87 @@ __global__ __launch_bounds__(256) void delta_entries(const Entry *__restrict__ e
     const int64_t column = e.id - from;
     if (e.id < 0 || column < 0 || column >= columns) return;
     const float z = picked[token * count + e.place];
-    delta[row * piece + column] = T((lifted<T>(z * inverse, lse[row]) - shares[k] * float(1 << lift_of<T>)) * factor[row]);
+    const float d = (lifted<T>(z * inverse, lse[row]) - shares[k] * float(1 << lift_of<T>)) * factor[row];
+    const D upper = D(d);
+    delta[row * piece + column] = upper;
+    if (LOWER) delta[(row + lower_rows(header->count)) * piece + column] = D(d - float(upper));
+}
+
+// The hidden states of d's two parts: the rows that count, in two sections with zeros behind them, and their header.  A block per row.
+template <typename T>
+__global__ __launch_bounds__(256) void split_rows(const Header *header, Hidden<T> hidden, T *__restrict__ rows, int64_t pitch, Header *both)
+{
+    const int64_t count = header->count, lower = lower_rows(count), row = blockIdx.x;
+    if (row == 0 && threadIdx.x == 0) *both = Header{int32_t(2 * lower), header->unscale};
+    if (row >= 2 * lower) return;
+    const int64_t from = row % lower;
+    const T *const source = hidden.of(count);
+    if (source == rows && row < count) return;           // (it is there already)
+    copy_row(from < count ? source + from * pitch : static_cast<const T *>(nullptr), pitch, rows + row * pitch, pitch, int(threadIdx.x), 256);
+}
+
+// bfloat16 to binary16, whose smaller range takes what is multiplied by a power of two, exactly: one that brings the largest magnitude into [2^14, 2^15).
+// Then everything down to 2^-31 of the largest keeps its eight bits.  The first pass converts with a guess of that power, and remembers the largest
+// magnitude its blocks saw; the second one converts again only where that did not come into [2^3, 2^15): down to 2^-20 of the largest all bits are kept then.
+// 8192 x 2048 hidden states and 50257 x 2048 weights: bound by memory, and a launch that finds nothing to do.
+struct Conversion {
+    const __bf16 *from;
+    _Float16 *to;
+    int64_t pieces;          // of 16 bytes, at most
+    float *most, *scale;
+    int guess;
+};
+constexpr int kHiddenGuess = 4, kWeightGuess = 10;   // largest hidden states of 2^-1 to 2^11, weights of 2^-7 to 2^5
+__device__ __forceinline__ float finite_magnitude(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
+__device__ __forceinline__ float block_most(float v)
+{
+    __shared__ float waves[4];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    __syncthreads();
+    return v;
+}
+// `hidden` (or null): the first blocks' rows, as many as count, in whole steps; the others' are the weight's.
+template <bool AGAIN>
+__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, Conversion rows, Conversion weight)
+{
+    typedef __bf16 From __attribute__((ext_vector_type(8)));
+    typedef _Float16 To __attribute__((ext_vector_type(8)));
+    const auto convert = [&](const Conversion &c, const __bf16 *source, int64_t pieces) {
+        int shift = c.guess;
+        if (AGAIN) {
+            float v = 0.f;
+            for (int k = int(threadIdx.x); k < kConvertBlocks; k += 256) v = fmaxf(v, c.most[k]);
+            v = block_most(v);
+            const bool again = v > 0.f && !(ilogbf(v) + shift >= 3 && ilogbf(v) + shift < 15);
+            if (again) shift = 14 - ilogbf(v);
+            if (blockIdx.x == 0 && threadIdx.x == 0) *c.scale = ldexpf(1.f, -shift);
+            if (!again) return;
+        }
+        float most = 0.f;
+        for (int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x; k < pieces; k += int64_t(kConvertBlocks) * 256) {
+            const From v = reinterpret_cast<const From *>(source)[k];
+            To out;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float x = float(v[e]);
+                if (!AGAIN) most = fmaxf(most, finite_magnitude(x));
+                out[e] = _Float16(ldexpf(x, shift));
+            }
+            reinterpret_cast<To *>(c.to)[k] = out;
+        }
+        if (AGAIN) return;
+        most = block_most(most);
+        if (threadIdx.x == 0) c.most[blockIdx.x] = most;
+    };
+    if (rows.to) {
+        const int64_t count = header->count;
+        convert(rows, hidden.of(count), lower_rows(count) * pitch / 8);
+    }
+    convert(weight, weight.from, weight.pieces);
 }
 
 Teacher teacher_of(const DistillLayout &l, const DistillBuffers &b)
@@ -326,22 +406,49 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
     return error;
 }
 
-template <typename T>
+template <typename T, typename D>
 hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const float *lse, const float *picked, const float *dloss, void *dhidden,
                        void *dweight, hipStream_t stream)
 {
     const HeadBuffers h = head_of(l, b);
     const float inverse = teacher_of(l, b).inverse;
-    const Calls<T, Tempered> calls{l.head, h, stream, Tempered{inverse}};
+    Calls<T, Tempered, D> calls{l.head, h, stream, Tempered{inverse}};
+    const auto at = [&](size_t offset) { return b.workspace + offset; };
+    calls.lower = l.lower;
+    if constexpr (calls.kOther) {
+        calls.hidden_of_products = reinterpret_cast<D *>(at(l.hidden16));
+        calls.weight_of_products = reinterpret_cast<D *>(at(l.weight16));
+        calls.scales = reinterpret_cast<float *>(at(l.scales));
+    }
     hipError_t error = l.head.tokens ? rows<true>(l, b, stream) : hipSuccess;
     const int64_t all = l.head.tokens * l.entries;
-    const hipError_t rest = calls.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), inverse, [&](int64_t first, int64_t columns) {
-        delta_entries<T><<<dim3(uint32_t((all + 255) / 256)), 256, 0, stream>>>(
-            calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
-            calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns,
-            calls.template at<T>(l.head.delta), l.head.piece);
+    const auto listed = [&] {
+        if (!l.lower || !l.head.tokens) return;
+        split_rows<T><<<dim3(uint32_t(calls.product_rows())), 256, 0, stream>>>(calls.header(), calls.hidden(), calls.template at<T>(l.head.hidden), l.head.pitch,
+                                                                               calls.products());
         calls.launched();
-    });
+    };
+    const auto entries = [&](const T *w, int64_t first, int64_t columns) {
+        const auto go = [&](auto in_two) {
+            delta_entries<T, D, decltype(in_two)::value><<<dim3(uint32_t((all + 255) / 256)), 256, 0, stream>>>(
+                calls.header(), calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
+                calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns,
+                calls.template at<D>(l.head.delta), l.head.piece);
+            calls.launched();
+        };
+        if (l.lower) go(std::true_type());
+        else go(std::false_type());
+        if constexpr (calls.kOther) {
+            float *const most = reinterpret_cast<float *>(at(l.most));
+            const Conversion rows{nullptr, first == 0 ? calls.hidden_of_products : nullptr, 0, most, calls.scales, kHiddenGuess};
+            const Conversion weight{w, calls.weight_of_products, columns * l.head.pitch / 8, most + kConvertBlocks, calls.scales + 1, kWeightGuess};
+            convert_rows<false><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, rows, weight);
+            calls.launched();
+            convert_rows<true><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, rows, weight);
+            calls.launched();
+        }
+    };
+    const hipError_t rest = calls.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), inverse, listed, entries);
     return error != hipSuccess ? error : rest;
 }
 
@@ -360,9 +467,10 @@ int launch_distill_grad(const DistillLayout &l, const DistillBuffers &b, const f
                         void *dhidden, void *dweight, void *stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (l.head.dt == CGX_F32) return gradient_of<float>(l, b, lse, picked, dloss, dhidden, dweight, s);
-    if (l.head.dt == CGX_F16) return gradient_of<_Float16>(l, b, lse, picked, dloss, dhidden, dweight, s);
-    return gradient_of<__bf16>(l, b, lse, picked, dloss, dhidden, dweight, s);
+    if (l.head.dt == CGX_F32) return gradient_of<float, float>(l, b, lse, picked, dloss, dhidden, dweight, s);
+    if (l.head.dt == CGX_F16) return gradient_of<_Float16, _Float16>(l, b, lse, picked, dloss, dhidden, dweight, s);
+    if (l.other) return gradient_of<__bf16, _Float16>(l, b, lse, picked, dloss, dhidden, dweight, s);
+    return gradient_of<__bf16, __bf16>(l, b, lse, picked, dloss, dhidden, dweight, s);
 }
 
 }  // namespace cgx

@@ -700,6 +700,9 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tok
 
 // ---------------------------------------------------------------- gradient
 
+// From the upper parts of d to the lower ones, in rows: whole tiles of 64, and whole steps of the products that sum over them.
+__host__ __device__ __forceinline__ int64_t lower_rows(int64_t count) { return (count + 63) / 64 * 64; }
+
 // d of a tile of a piece: logits as above, then dloss (exp(z - lse) - [v = target]) in its units, in the operands' type.
 // Every element of the piece's whole tiles is written; those of no token or no column are zeros.
 // d is rounded to the operands' type once, because the products that follow read it from the matrix cores' operands: its relative error,
@@ -709,15 +712,17 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tok
 // Forming the logits again costs 2 N V H operations and saves 4 N V bytes written and read by the loss and N V bytes of workspace that would have
 // to live from one call to the other.
 // 8192 tokens x 2048 x 25344 columns, bfloat16: 709 us = 1.20 PFLOP/s, with 0.41 GB written at the tiles' ends while no products run.
-template <typename K, typename S>
+//
+// D: the type that d is held in, where that is not the operands' (see Calls).  LOWER: what rounding takes from d is held as well, lower_rows(count) rows on.
+template <typename K, typename S, typename D, bool LOWER>
 __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                            int64_t pitch, int64_t first, int64_t columns,
                                                            const int32_t *__restrict__ target, const float *__restrict__ lse,
-                                                           const float *__restrict__ factor, typename K::T *__restrict__ delta, int64_t piece, S softmax)
+                                                           const float *__restrict__ factor, D *__restrict__ delta, int64_t piece, S softmax)
 {
     using T = typename K::T;
     __shared__ __align__(256) Lds<K> lds;
-    const int64_t count = header->count;
+    const int64_t count = header->count, lower = lower_rows(count);
     int tm, tn;
     if (!tile_of_block(blockIdx.x, ~0u, up(count, K::BM), up(columns, K::BN), tm, tn)) return;
     const int64_t m0 = int64_t(tm) * K::BM, n0 = int64_t(tn) * K::BN;
@@ -733,32 +738,40 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
     const int g = tile.lane >> 4, r = tile.lane & 15;
     const int64_t c0 = n0 + tile.wn + 16 * g;
     const bool whole = m0 + K::BM <= count && n0 + K::BN <= columns;
-    constexpr int kPer = 16 / int(sizeof(T));
-    typedef T Vec __attribute__((ext_vector_type(kPer)));
+    constexpr int kPer = 16 / int(sizeof(D));
+    typedef D Vec __attribute__((ext_vector_type(kPer)));
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
         const bool counts = row < count;
         const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] : 0.f;
         const int64_t hit = S::kTargets && counts ? int64_t(target[row]) - first - c0 : -1;
-        T *const out = delta + row * piece + c0;
+        D *const out = delta + row * piece + c0;
 #pragma unroll
         for (int k = 0; k < 16; k += kPer) {
-            Vec v;
+            Vec v, rest;
 #pragma unroll
-            for (int e = 0; e < kPer; e++) v[e] = T(lifted<T>(softmax.of(tile.acc[i][(k + e) / 4][(k + e) % 4]), base) * f);
+            for (int e = 0; e < kPer; e++) {
+                const float d = lifted<T>(softmax.of(tile.acc[i][(k + e) / 4][(k + e) % 4]), base) * f;
+                v[e] = D(d);
+                if (LOWER) rest[e] = D(d - float(v[e]));
+            }
             if (!whole)
 #pragma unroll
                 for (int e = 0; e < kPer; e++)
-                    if (!counts || c0 + k + e >= columns) v[e] = T(0.f);
+                    if (!counts || c0 + k + e >= columns) {
+                        v[e] = D(0.f);
+                        if (LOWER) rest[e] = D(0.f);
+                    }
             *reinterpret_cast<Vec *>(out + k) = v;
+            if (LOWER) *reinterpret_cast<Vec *>(out + lower * piece + k) = rest;
         }
         if (S::kTargets && hit >= 0 && hit < 16) {
             float z = 0.f;
 #pragma unroll
             for (int k = 0; k < 16; k++)
                 if (hit == k) z = tile.acc[i][k / 4][k % 4];
-            out[hit] = T((lifted<T>(z, base) - float(1 << lift_of<T>)) * f);
+            out[hit] = D((lifted<T>(z, base) - float(1 << lift_of<T>)) * f);
         }
     }
 }
@@ -789,10 +802,11 @@ __device__ __forceinline__ f32x4 joined(const float *first, int64_t apart, uint3
 
 // dx += d W over a piece, in binary32.  accumulate: not the first piece.  W is read along its rows, as stored; the matrix cores want its
 // columns, and transposing LDS reads give them (Side::fragment).  8192 x 25344 columns x 2048, bfloat16: 616 us = 1.38 PFLOP/s.
-template <typename K>
+// SCALED: the product is also multiplied by *scale.
+template <typename K, bool SCALED>
 __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *header, const typename K::T *delta, int64_t piece,
                                                             const typename K::T *weight, int64_t pitch, int64_t columns, int32_t blocks,
-                                                            int32_t accumulate, float *__restrict__ sums)
+                                                            int32_t accumulate, float *__restrict__ sums, const float *scale)
 {
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
@@ -814,6 +828,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
     tile.run(a, b, steps, int(left < K::kDepth ? left : K::kDepth), lds);
     const int g = tile.lane >> 4, r = tile.lane & 15;
     float *const own = sums + int64_t(part) * count * pitch;
+    const float by = SCALED ? *scale : 1.f;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
@@ -823,7 +838,8 @@ __global__ __launch_bounds__(K::kThreads, 2) void hidden_tiles(const Header *hea
             const int64_t column = n0 + tile.wn + 16 * j + 4 * g;
             if (column >= pitch) continue;
             f32x4 *p = reinterpret_cast<f32x4 *>(own + row * pitch + column);
-            *p = accumulate ? *p + tile.acc[i][j] : tile.acc[i][j];
+            const f32x4 v = SCALED ? tile.acc[i][j] * by : tile.acc[i][j];
+            *p = accumulate ? *p + v : v;
         }
     }
 }
@@ -863,10 +879,11 @@ __device__ __forceinline__ void store_weights(T *dweight, int64_t row, int64_t c
     }
 }
 
-template <typename K>
+template <typename K, typename OUT, bool SCALED>
 __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *header, const typename K::T *delta, int64_t piece,
                                                             Hidden<typename K::T> hidden, int64_t pitch, int64_t columns, int64_t width,
-                                                            int32_t blocks, typename K::T *__restrict__ dweight, float *__restrict__ spare)
+                                                            int32_t blocks, OUT *__restrict__ dweight, float *__restrict__ spare,
+                                                            const float *scale)
 {
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count;
@@ -903,7 +920,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *hea
                 *reinterpret_cast<f32x4 *>(own + (tile.wm + 16 * i + l) * K::BN + tile.wn + 16 * j + 4 * g) = tile.acc[i][j];
         return;
     }
-    const float unscale = header->unscale;
+    const float unscale = SCALED ? header->unscale * *scale : header->unscale;
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + l;
@@ -917,9 +934,9 @@ __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *hea
 }
 
 // The tiles of weight_tiles' last round from their parts: a block per 16 rows of a tile.
-template <typename K>
+template <typename K, typename OUT, bool SCALED>
 __global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t columns, int64_t width, int32_t blocks,
-                                                   typename K::T *__restrict__ dweight, const float *__restrict__ spare)
+                                                   OUT *__restrict__ dweight, const float *__restrict__ spare, const float *scale)
 {
     constexpr int kStrip = 16;
     const uint32_t tiles_m = up(columns, K::BM), tiles_n = up(width, K::BN);
@@ -927,7 +944,7 @@ __global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t
     const uint32_t at = blockIdx.x / (K::BM / kStrip), strip = blockIdx.x % (K::BM / kStrip);
     int tm, tn;
     if (at >= r.rest || !tile_of_block(r.whole + at, r.whole, tiles_m, tiles_n, tm, tn)) return;
-    const float unscale = header->unscale;
+    const float unscale = SCALED ? header->unscale * *scale : header->unscale;
     for (int k = int(threadIdx.x) * 4; k < kStrip * K::BN; k += 1024) {
         const int m = int(strip) * kStrip + k / K::BN, n = k % K::BN;
         const int64_t row = int64_t(tm) * K::BM + m, column = int64_t(tn) * K::BN + n;
@@ -940,7 +957,8 @@ __global__ __launch_bounds__(256) void weight_rest(const Header *header, int64_t
 // dhidden from the sums, in their units; a block per token.  side, steps: of the kernel that left them.  Bound by memory: 8192 x 2048
 // binary32 sums to bfloat16 23 us (101 MB, 4.4 TB/s); 4096 tokens of 768, the 15 % that
 // count in 28 parts (their nine tiles, over 256 compute units: 53 MB), 12.5 us.
-template <typename T>
+// LOWER: the header counts both parts' rows, and the sums of the lower part are half as many rows on.
+template <typename T, bool LOWER>
 __global__ __launch_bounds__(256) void round_hidden(const Header *header, const int32_t *__restrict__ place, const float *__restrict__ sums,
                                                     int64_t pitch, int64_t width, int32_t side, int32_t steps, int32_t blocks,
                                                     T *__restrict__ dhidden)
@@ -954,7 +972,8 @@ __global__ __launch_bounds__(256) void round_hidden(const Header *header, const 
     const float *s = sums + int64_t(row < 0 ? 0 : row) * pitch;
     T *d = dhidden + token * width;
     for (int64_t k = int64_t(threadIdx.x) * 4; k < width; k += 1024) {
-        const f32x4 v = row < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : joined(s + k, count * pitch, parts);
+        f32x4 v = row < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : joined(s + k, count * pitch, parts);
+        if (LOWER && row >= 0) v += joined(s + count / 2 * pitch + k, count * pitch, parts);
         Four out;
 #pragma unroll
         for (int e = 0; e < 4; e++) out[e] = T(v[e] * unscale);
@@ -1007,7 +1026,12 @@ Size size_of(int64_t rows, int64_t columns, int64_t split = 0)
     return large <= small && large <= tiny ? kLarge : small <= tiny ? kSmall : kTiny;
 }
 
-template <typename T, typename S = Targets>
+// d is rounded to 16 bits where the operands have 16.  A target's element, which is most of a row, is near 1 in the units that d is held in and loses
+// little; a teacher's entries may be anything.  So the calls of Tempered hold d of few tokens, whose products are bound by reading and writing the
+// weights, in two parts of 16 bits (lower: two sections of rows, with the hidden states in both), and that of more bfloat16
+// tokens in binary16, against hidden states and weights in binary16 (D; multiplied by a power of two that brings the largest close to that type's
+// largest, so that what bfloat16 holds is held to 2^-32 of it).
+template <typename T, typename S = Targets, typename D = T>
 struct Calls {
     const HeadLayout &l;
     const HeadBuffers &b;
@@ -1015,6 +1039,10 @@ struct Calls {
     S softmax = S();
     typename S::Picks picks = typename S::Picks();
     int32_t *tokens_of_rows = nullptr;
+    bool lower = false;
+    D *hidden_of_products = nullptr, *weight_of_products = nullptr;        // where D is another type
+    float *scales = nullptr;                                               // of the hidden states, of the weight's piece: 1 / the power of two
+    static constexpr bool kOther = !std::is_same<D, T>::value;
     mutable hipError_t error = hipSuccess;      // of the first launch that was refused
 
     void launched() const
@@ -1046,7 +1074,7 @@ struct Calls {
         const int64_t columns = l.padded && l.tokens ? l.columns(0) : 0, wanted = (columns + kListThreads / 64 - 1) / (kListThreads / 64);
         const int64_t pads = wanted < 8 * kHeadBlocks ? wanted : 8 * kHeadBlocks;
         list_tokens<T><<<dim3(uint32_t(grid + pads)), kListThreads, 0, stream>>>(
-            b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, l.dt == CGX_F16 ? 14 : l.dt == CGX_BF16 ? kLift : 0,
+            b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, std::is_same<D, _Float16>::value ? 14 : std::is_same<D, __bf16>::value ? kLift : 0,
             outer, static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, int32_t(head_depth(l.dt)), h.own ? 1 : 0, header(),
             Lists{at<int32_t>(l.place), at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), tokens_of_rows}, uint32_t(grid),
             Padding<T>{static_cast<const T *>(b.weight), at<T>(l.weight), columns, l.width, l.pitch});
@@ -1140,81 +1168,110 @@ struct Calls {
     template <typename K>
     void delta(const T *w, int64_t first, int64_t columns) const
     {
-        delta_tiles<K, S><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
-            header(), hidden(), w, l.pitch, first, columns, at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), at<T>(l.delta),
-            l.piece, softmax);
-        launched();
+        const auto go = [&](auto in_two) {
+            delta_tiles<K, S, D, decltype(in_two)::value><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
+                header(), hidden(), w, l.pitch, first, columns, at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), at<D>(l.delta),
+                l.piece, softmax);
+            launched();
+        };
+        if constexpr (!S::kTargets && !kOther && sizeof(T) == 2 && K::BM < 256) {
+            if (lower) return go(std::true_type());
+        }
+        go(std::false_type());
+    }
+    // What the products of d run over: the rows that count, or (lower) two sections of them.
+    Header *products() const { return header() + (lower ? 1 : 0); }
+    int64_t product_rows() const { return lower ? 2 * lower_rows(l.tokens) : l.tokens; }
+    Hidden<D> product_hidden() const
+    {
+        if constexpr (kOther) return Hidden<D>{nullptr, hidden_of_products, l.tokens};
+        else {
+            const Hidden<T> h = hidden();
+            return Hidden<D>{lower ? nullptr : h.own, h.listed, l.tokens};
+        }
     }
     // The tile of dx: its sum over the vocabulary is split where there are few of it, so that any size fills the chip, and each part is written
     // and read again.  The larger tile, then, where it needs few parts.  Whole calls with large and with small tiles, us: 2048 x 1024 x 50257 (32
     // large tiles) 846 and 896, 600 x 2048 x 50257 (24) 629 and 619, 1500 x 768 x 30522 (18) 346 and 344.
     Size sums_size() const
     {
-        if (sizeof(T) == 4 || l.tokens <= 64) return kTiny;
+        if (sizeof(T) == 4 || product_rows() <= 64) return kTiny;
         const auto blocks_of = [&](int side, int64_t most) {
-            const int64_t n = tiles(l.tokens, l.pitch, side), parts = l.piece / (kLeastSteps * head_depth(l.dt));
+            const int64_t n = tiles(product_rows(), l.pitch, side), parts = l.piece / (kLeastSteps * head_depth(l.dt));
             return n * (most / n < 1 ? 1 : most / n < parts ? most / n : parts);
         };
-        if (tiles(l.tokens, l.pitch, 256) >= 32 && blocks_of(256, blocks<Large<T, kSumContiguous, kRowContiguous>>) >= 192) return kLarge;
+        if (tiles(product_rows(), l.pitch, 256) >= 32 && blocks_of(256, blocks<Large<T, kSumContiguous, kRowContiguous>>) >= 192) return kLarge;
         return blocks_of(128, 2 * kHeadBlocks) >= 384 ? kSmall : kTiny;
     }
     template <typename K>
-    void hidden_sums(const T *w, int64_t first, int64_t columns) const
+    void hidden_sums(const D *w, int64_t first, int64_t columns) const
     {
-        const int64_t n = tiles(l.tokens, l.pitch, K::BM);
-        hidden_tiles<K><<<dim3(uint32_t(n > blocks<K> ? n : blocks<K>)), K::kThreads, 0, stream>>>(
-            header(), at<T>(l.delta), l.piece, w, l.pitch, columns, blocks<K>, first > 0, at<float>(l.sums));
+        const int64_t n = tiles(product_rows(), l.pitch, K::BM);
+        hidden_tiles<K, kOther><<<dim3(uint32_t(n > blocks<K> ? n : blocks<K>)), K::kThreads, 0, stream>>>(
+            products(), at<D>(l.delta), l.piece, w, l.pitch, columns, blocks<K>, first > 0, at<float>(l.sums), kOther ? scales + 1 : nullptr);
         launched();
     }
     template <typename K>
     void rounded(T *dhidden) const
     {
-        round_hidden<T><<<dim3(uint32_t(l.tokens)), 256, 0, stream>>>(header(), at<int32_t>(l.place), at<float>(l.sums), l.pitch, l.width,
-                                                                   K::BM, int32_t((l.piece + K::kDepth - 1) / K::kDepth), blocks<K>,
-                                                                   dhidden);
-        launched();
+        const auto go = [&](auto in_two) {
+            round_hidden<T, decltype(in_two)::value><<<dim3(uint32_t(l.tokens)), 256, 0, stream>>>(
+                products(), at<int32_t>(l.place), at<float>(l.sums), l.pitch, l.width, K::BM, int32_t((l.piece + K::kDepth - 1) / K::kDepth), blocks<K>,
+                dhidden);
+            launched();
+        };
+        if constexpr (!S::kTargets && !kOther && sizeof(T) == 2) {
+            if (lower) return go(std::true_type());
+        }
+        go(std::false_type());
     }
     template <typename K>
     void weight_rows(int64_t first, int64_t columns, T *dweight) const
     {
         const int64_t n = tiles(columns, l.width, K::BM), rest = n % blocks<K>;
         // (whether the rest is split depends on how many tokens count, too)
-        weight_tiles<K><<<dim3(uint32_t(n - rest + (rest ? blocks<K> : 0))), K::kThreads, 0, stream>>>(
-            header(), at<T>(l.delta), l.piece, hidden(), l.pitch, columns, l.width, blocks<K>, dweight + first * l.width, at<float>(l.spare));
+        weight_tiles<K, T, kOther><<<dim3(uint32_t(n - rest + (rest ? blocks<K> : 0))), K::kThreads, 0, stream>>>(
+            products(), at<D>(l.delta), l.piece, product_hidden(), l.pitch, columns, l.width, blocks<K>, dweight + first * l.width,
+            at<float>(l.spare), scales);
         launched();
-        if (!rest || 2 * rest > blocks<K> || (l.tokens + K::kDepth - 1) / K::kDepth < 2 * kLeastSteps) return;
-        weight_rest<K><<<dim3(uint32_t(rest * (K::BM / 16))), 256, 0, stream>>>(header(), columns, l.width, blocks<K>,
-                                                                             dweight + first * l.width, at<float>(l.spare));
+        if (!rest || 2 * rest > blocks<K> || (product_rows() + K::kDepth - 1) / K::kDepth < 2 * kLeastSteps) return;
+        weight_rest<K, T, kOther><<<dim3(uint32_t(rest * (K::BM / 16))), 256, 0, stream>>>(products(), columns, l.width, blocks<K>,
+                                                                                        dweight + first * l.width, at<float>(l.spare), scales);
         launched();
     }
-    // entries(first, columns): queues what d of a piece lacks.
-    template <class Entries>
-    hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight, float outer, Entries entries) const
+    // listed(): queues what the products' hidden states need once the tokens are listed; entries(w, first, columns): what d of a piece lacks, and what the
+    // products' weights need.
+    template <class Listed, class Entries>
+    hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight, float outer, Listed listed, Entries entries) const
     {
         list(dloss, lse, outer);
+        listed();
         const Size sums = sums_size();
         for (int64_t k = 0; k < l.pieces; k++) {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
             if (l.tokens) {
-                const Size size = size_of<T>(l.tokens, columns);
+                const Size size = lower ? kTiny : size_of<T>(l.tokens, columns);
                 if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                entries(first, columns);
-                if (sums == kLarge) hidden_sums<Large<T, kSumContiguous, kRowContiguous>>(w, first, columns);
-                else if (sums == kSmall) hidden_sums<Small<T, kSumContiguous, kRowContiguous>>(w, first, columns);
-                else hidden_sums<Tiny<T, kSumContiguous, kRowContiguous>>(w, first, columns);
+                entries(w, first, columns);
+                const D *of;
+                if constexpr (kOther) of = weight_of_products;
+                else of = w;
+                if (sums == kLarge) hidden_sums<Large<D, kSumContiguous, kRowContiguous>>(of, first, columns);
+                else if (sums == kSmall) hidden_sums<Small<D, kSumContiguous, kRowContiguous>>(of, first, columns);
+                else hidden_sums<Tiny<D, kSumContiguous, kRowContiguous>>(of, first, columns);
             }
-            const Size size = size_of<T>(columns, l.width, (l.tokens + head_depth(l.dt) - 1) / head_depth(l.dt));
-            if (size == kLarge) weight_rows<Large<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
-            else if (size == kSmall) weight_rows<Small<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
-            else weight_rows<Tiny<T, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            const Size size = size_of<T>(columns, l.width, (product_rows() + head_depth(l.dt) - 1) / head_depth(l.dt));
+            if (size == kLarge) weight_rows<Large<D, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            else if (size == kSmall) weight_rows<Small<D, kRowContiguous, kRowContiguous>>(first, columns, dweight);
+            else weight_rows<Tiny<D, kRowContiguous, kRowContiguous>>(first, columns, dweight);
         }
         if (!l.tokens) return error;
-        if (sums == kLarge) rounded<Large<T, kSumContiguous, kRowContiguous>>(dhidden);
-        else if (sums == kSmall) rounded<Small<T, kSumContiguous, kRowContiguous>>(dhidden);
-        else rounded<Tiny<T, kSumContiguous, kRowContiguous>>(dhidden);
+        if (sums == kLarge) rounded<Large<D, kSumContiguous, kRowContiguous>>(dhidden);
+        else if (sums == kSmall) rounded<Small<D, kSumContiguous, kRowContiguous>>(dhidden);
+        else rounded<Tiny<D, kSumContiguous, kRowContiguous>>(dhidden);
         return error;
     }
 };

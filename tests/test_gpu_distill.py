@@ -7,7 +7,9 @@ Tolerances follow from the arithmetic.  With u the unit roundoff of the operands
   q: relative, exp of a difference (2^-23 and 2^-23 of the magnitudes in it) and a sum of at most 1024 terms in 64 lanes (22 * 2^-24)
   loss: those of q, of lse and of picked in its terms, the terms' own roundings (2^-22 of the magnitudes in them), sums of `entries` terms
   d: relative 2 (e / T + 2^-23 |z| / T) + 1.2e-5 + 2^-23 |lse| of its probability, q's error, 2^-23 of both for the difference, and u of
-  itself where it is rounded to the operands' type (binary16: at least half a subnormal step under the scale, 2^-39 of the largest factor)
+  itself where it is rounded to the operands' type or a finer one (binary16, which also holds that of many bfloat16 tokens: at least half a
+  subnormal step under the scale, 2^-39 of the largest factor)
+  operands in binary16 instead of bfloat16: half a subnormal step under their power of two, 2^-25 / 2^3 of the largest magnitude
   its products: the same weighted by the other operand, binary32 sums of n terms (n 2^-24), and u of the result.
 """
 import math
@@ -125,13 +127,14 @@ def check(torch, hidden, weight, ids, teacher, dloss=None, temperature=1.0, igno
     at_entries, off_entries = torch.zeros_like(p).scatter_add_(1, at, q), torch.zeros_like(p).scatter_add_(1, at, q * off_q)
     d = g * (p - at_entries)
     x = torch.where(kept, x, 0.0)
-    smallest = 2.0**-39 * float(dloss.abs().max()) if name == "f16" and len(dloss) else 0.0
+    smallest = 2.0**-39 * float(dloss.abs().max()) if name != "f32" and len(dloss) else 0.0
+    step = 2.0**-28 if name == "bf16" else 0.0
     off = g.abs() * (p * (2 * off_z + 1.2e-5 + 2.0**-22 * (1 + lse.abs())) + off_entries + 2.0**-23 * (p + at_entries)) * 1.01 + u * d.abs() + smallest
     off = torch.where(kept, off, 0.0)
     least = 2.0**-25 if name == "f16" else 1e-38
     dx, dw = torch.mm(d, w) / t, torch.mm(d.t().contiguous(), x) / t
-    bx = torch.mm(off + (vocab + 8) * 2.0**-24 * d.abs(), w.abs()) * 1.01 / t + (u + 2.0**-22) * dx.abs() + least
-    bw = torch.mm((off + (len(rows) + 8) * 2.0**-24 * d.abs()).t().contiguous(), x.abs()) * 1.01 / t + (u + 2.0**-22) * dw.abs() + least
+    bx = torch.mm(off + (vocab + 8) * 2.0**-24 * d.abs(), w.abs() + step * w.abs().max()) * 1.01 / t + step * d.abs().sum(dim=1, keepdim=True) * w.abs().max() / t + (u + 2.0**-22) * dx.abs() + least
+    bw = torch.mm((off + (len(rows) + 8) * 2.0**-24 * d.abs()).t().contiguous(), x.abs()) * 1.01 / t + (step * x.abs().max() * d.abs().sum(dim=0)[:, None] / t if len(rows) else 0.0) + (u + 2.0**-22) * dw.abs() + least
     assert ((got["dhidden"][rows].double() - dx).abs() <= bx).all()
     assert ((got["dweight"].double() - dw).abs() <= bw).all()
     return got
@@ -343,3 +346,43 @@ def test_captured_and_replayed(torch, tokens):
         want = call(torch, hidden, weight, ids, teacher, dloss, temperature=3.0)
         for what, t in (("loss", loss), ("lse", lse), ("picked", picked), ("dhidden", dhidden), ("dweight", dweight)):
             assert torch.equal(t, want[what]), what
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 3, 64, 65, 128, 129, 1000])
+def test_gradients_are_about_as_exact_as_their_type(torch, tokens, dtype):
+    """In the 2-norm, against the exact gradients rounded once.  d in two parts, or in binary16 for bfloat16, adds at most 2^-3 of a rounding to each
+    element, 2^-6 to its square; that of many binary16 tokens is rounded once itself, and adds another one: sqrt(2), and what the mantissas of a few
+    hundred large elements do to it."""
+    hidden, weight, ids, teacher = inputs(torch, tokens, 200, 3000, 24, dtype, seed=31, marked=0.1)
+    hidden = (hidden.float() * 2).to(hidden.dtype)
+    dloss = torch.full((tokens,), 1 / 3, device="cuda")
+    got = call(torch, hidden, weight, ids, teacher, dloss)
+    there, x, w = ids != -100, hidden.double(), weight.double()
+    at = ids.clamp(min=0)
+    q = torch.nan_to_num(torch.softmax(torch.where(there, teacher.double(), -math.inf), dim=1))
+    d = torch.softmax(torch.mm(x, w.t()), dim=1).scatter_add_(1, at, -q) * dloss.double()[:, None] * there.any(dim=1)[:, None]
+    most = 1.6 if dtype == "f16" and tokens > 128 else 1.05
+    for got_, want in ((got["dhidden"], torch.mm(d, w)), (got["dweight"], torch.mm(d.t().contiguous(), x))):
+        once = float((want.to(got_.dtype).double() - want).norm())
+        assert float((got_.double() - want).norm()) <= most * once
+
+
+@pytest.mark.parametrize("tokens", [100, 300])
+@pytest.mark.parametrize("of_hidden, of_weight", [(2.0**30, 2.0**-30), (2.0**-40, 2.0**40), (2.0**-100, 1.0), (1.0, 2.0**-100), (2.0**9, 2.0**-9)])
+def test_operands_of_any_size_in_bfloat16(torch, tokens, of_hidden, of_weight):
+    """Powers of two change nothing but the results' own power where the logits stay what they are, and next to nothing where these vanish."""
+    hidden, weight, ids, teacher = inputs(torch, tokens, 136, 900, 12, "bf16", seed=3)
+    dloss = torch.full((tokens,), 0.5, device="cuda")
+    check(torch, (hidden.float() * of_hidden).bfloat16(), (weight.float() * of_weight).bfloat16(), ids, teacher, dloss)
+    weight.zero_()
+    check(torch, hidden, weight, ids, teacher, dloss)
+
+
+def test_operands_with_outliers_in_bfloat16(torch):
+    hidden, weight, ids, teacher = inputs(torch, 300, 136, 900, 12, "bf16", seed=3)
+    hidden[:, 7] *= 0.0
+    hidden[11, 7] = 2.0**20
+    weight[:, 7] *= 2.0**-20
+    weight[5, 9] = 24.0
+    check(torch, hidden, weight, ids, teacher, torch.full((300,), 0.5, device="cuda"))
