@@ -239,25 +239,36 @@ __global__ __launch_bounds__(64 * kGatherWaves) void join_gathered(Teacher teach
 }
 
 // d at the teacher's entries within a piece of the vocabulary, in its units: a thread per entry.
+struct Entries {
+    const Entry *entries;
+    const float *shares;
+    int32_t count;           // a token
+    int64_t all;
+    const int32_t *place;
+    const float *lse, *factor, *picked;
+    float inverse;
+    int64_t from, columns, piece;
+};
 template <typename T, typename D, bool LOWER>
-__global__ __launch_bounds__(256) void delta_entries(const Header *header, const Entry *__restrict__ entries, const float *__restrict__ shares,
-                                                     int32_t count, int64_t all, const int32_t *__restrict__ place, const float *__restrict__ lse,
-                                                     const float *__restrict__ factor, const float *__restrict__ picked, float inverse, int64_t from,
-                                                     int64_t columns, D *__restrict__ delta, int64_t piece)
+__device__ __forceinline__ void put_entry(const Entries &n, int64_t k, const Header *header, D *__restrict__ delta)
 {
-    const int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (k >= all) return;
-    const int64_t token = k / count;
-    const int32_t row = place[token];
+    if (k >= n.all) return;
+    const int64_t token = k / n.count;
+    const int32_t row = n.place[token];
     if (row < 0) return;                                 // (it may have no sorted entries)
-    const Entry e = entries[k];
-    const int64_t column = e.id - from;
-    if (e.id < 0 || column < 0 || column >= columns) return;
-    const float z = picked[token * count + e.place];
-    const float d = (lifted<T>(z * inverse, lse[row]) - shares[k] * float(1 << lift_of<T>)) * factor[row];
+    const Entry e = n.entries[k];
+    const int64_t column = e.id - n.from;
+    if (e.id < 0 || column < 0 || column >= n.columns) return;
+    const float z = n.picked[token * n.count + e.place];
+    const float d = (lifted<T>(z * n.inverse, n.lse[row]) - n.shares[k] * float(1 << lift_of<T>)) * n.factor[row];
     const D upper = D(d);
-    delta[row * piece + column] = upper;
-    if (LOWER) delta[(row + lower_rows(header->count)) * piece + column] = D(d - float(upper));
+    delta[row * n.piece + column] = upper;
+    if (LOWER) delta[(row + lower_rows(header->count)) * n.piece + column] = D(d - float(upper));
+}
+template <typename T, bool LOWER>
+__global__ __launch_bounds__(256) void delta_entries(const Header *header, Entries entries, T *__restrict__ delta)
+{
+    put_entry<T, T, LOWER>(entries, int64_t(blockIdx.x) * 256 + threadIdx.x, header, delta);
 }
 
 // The hidden states of d's two parts: the rows that count, in two sections with zeros behind them, and their header.  A block per row.
@@ -278,7 +289,6 @@ __global__ __launch_bounds__(256) void split_rows(const Header *header, Hidden<T
 // magnitude its blocks saw; the second one converts again only where that did not come into [2^3, 2^15): down to 2^-20 of the largest all bits are kept then.
 // 8192 x 2048 hidden states and 50257 x 2048 weights: bound by memory, and a launch that finds nothing to do.
 struct Conversion {
-    const __bf16 *from;
     _Float16 *to;
     int64_t pieces;          // of 16 bytes, at most
     float *most, *scale;
@@ -297,10 +307,17 @@ __device__ __forceinline__ float block_most(float v)
     __syncthreads();
     return v;
 }
-// `hidden` (or null): the first blocks' rows, as many as count, in whole steps; the others' are the weight's.
+// rows.to may be null: the hidden states are converted with the first piece of the weight.  The second pass' blocks behind the first kConvertBlocks see to
+// the teacher's entries.
 template <bool AGAIN>
-__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, Conversion rows, Conversion weight)
+__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, const __bf16 *__restrict__ source_weight, Conversion rows,
+                                                    Conversion weight,
+                                                    Entries entries, _Float16 *__restrict__ delta)
 {
+    if (AGAIN && blockIdx.x >= kConvertBlocks) {
+        put_entry<__bf16, _Float16, false>(entries, int64_t(blockIdx.x - kConvertBlocks) * 256 + threadIdx.x, header, delta);
+        return;
+    }
     typedef __bf16 From __attribute__((ext_vector_type(8)));
     typedef _Float16 To __attribute__((ext_vector_type(8)));
     const auto convert = [&](const Conversion &c, const __bf16 *source, int64_t pieces) {
@@ -334,7 +351,7 @@ __global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden
         const int64_t count = header->count;
         convert(rows, hidden.of(count), lower_rows(count) * pitch / 8);
     }
-    convert(weight, weight.from, weight.pieces);
+    convert(weight, source_weight, weight.pieces);
 }
 
 Teacher teacher_of(const DistillLayout &l, const DistillBuffers &b)
@@ -429,22 +446,21 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
         calls.launched();
     };
     const auto entries = [&](const T *w, int64_t first, int64_t columns) {
-        const auto go = [&](auto in_two) {
-            delta_entries<T, D, decltype(in_two)::value><<<dim3(uint32_t((all + 255) / 256)), 256, 0, stream>>>(
-                calls.header(), calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
-                calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns,
-                calls.template at<D>(l.head.delta), l.head.piece);
-            calls.launched();
-        };
-        if (l.lower) go(std::true_type());
-        else go(std::false_type());
+        const Entries n{calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
+                        calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns, l.head.piece};
+        const uint32_t blocks = uint32_t((all + 255) / 256);
         if constexpr (calls.kOther) {
             float *const most = reinterpret_cast<float *>(at(l.most));
-            const Conversion rows{nullptr, first == 0 ? calls.hidden_of_products : nullptr, 0, most, calls.scales, kHiddenGuess};
-            const Conversion weight{w, calls.weight_of_products, columns * l.head.pitch / 8, most + kConvertBlocks, calls.scales + 1, kWeightGuess};
-            convert_rows<false><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, rows, weight);
+            const Conversion rows{first == 0 ? calls.hidden_of_products : nullptr, 0, most, calls.scales, kHiddenGuess};
+            const Conversion weight{calls.weight_of_products, columns * l.head.pitch / 8, most + kConvertBlocks, calls.scales + 1, kWeightGuess};
+            D *const delta = calls.template at<D>(l.head.delta);
+            convert_rows<false><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
             calls.launched();
-            convert_rows<true><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, rows, weight);
+            convert_rows<true><<<dim3(kConvertBlocks + blocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
+            calls.launched();
+        } else {
+            if (l.lower) delta_entries<T, sizeof(T) == 2><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));
+            else delta_entries<T, false><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));
             calls.launched();
         }
     };
