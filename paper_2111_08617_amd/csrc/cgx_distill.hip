@@ -98,19 +98,16 @@ __device__ __forceinline__ void sort_keys(uint64_t *key, int lane)
 }
 
 template <int M, bool GRAD>
-__global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, int64_t tokens, int64_t *__restrict__ mark,
-                                                               Entry *__restrict__ entries, float *__restrict__ shares,
-                                                               uint16_t *__restrict__ strips, int64_t pitch)
+__device__ __forceinline__ TeacherRow row_entries(const Teacher &teacher, int64_t token, int lane, RowShared<M> &s, Entry *__restrict__ entries,
+                                                  float *__restrict__ shares, uint16_t *__restrict__ strips, int64_t pitch)
 {
-    __shared__ RowShared<M> all[kRowWaves];
-    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int64_t token = int64_t(blockIdx.x) * kRowWaves + wave;
-    if (token >= tokens) return;                         // (no barriers of blocks follow)
-    RowShared<M> &s = all[wave];
+    typedef uint32_t Four __attribute__((ext_vector_type(4)));
     const TeacherRow r = teacher_row(teacher, token, lane);
-    if (lane == 0) mark[token] = r.wrong ? kWrong : r.takes_part() ? kTakesPart : kNoPart;
-    if (!r.takes_part()) return;
     const int64_t first = token * teacher.entries;
+    uint16_t *const row = strips + token * pitch;
+    if (!GRAD && strips)                                 // (rows of strips are whole pieces of 16 bytes)
+        for (int64_t strip = lane * 8; strip < pitch; strip += 512) *reinterpret_cast<Four *>(row + strip) = Four(0u);
+    if (!r.takes_part()) return r;
     constexpr uint64_t kNone = ~uint64_t(0);
     for (int k = lane; k < M; k += 64) {
         uint64_t key = kNone;
@@ -138,13 +135,9 @@ __global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, 
         }
         entries[first + k] = e;
     }
-    if (GRAD || !strips) return;
-    // (of 8 at a time: rows of strips are whole pieces of 16 bytes)
-    typedef uint32_t Four __attribute__((ext_vector_type(4)));
-    uint16_t *const row = strips + token * pitch;
-    for (int64_t strip = lane * 8; strip < pitch; strip += 512) *reinterpret_cast<Four *>(row + strip) = Four(0u);
+    if (GRAD || !strips) return r;
     wave_fence();
-    // the first entry of a strip writes it, after the zeros: stores of a wave to one address are in order
+    // The first entry of a strip writes it, after the zeros: stores of a wave to one address are in order
     const auto strip_of = [](uint64_t key) { return int64_t(key >> kStripBits) / kStripColumns; };
     for (int k = lane; k < teacher.entries; k += 64) {
         const uint64_t key = s.key[k];
@@ -153,6 +146,77 @@ __global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, 
         while (n < kStripMost && k + int(n) < teacher.entries && s.key[k + n] != kNone && strip_of(s.key[k + n]) == strip_of(key)) n++;
         row[strip_of(key)] = uint16_t(uint32_t(k) | n << kStripBits);
     }
+    return r;
+}
+
+template <int M, bool GRAD>
+__global__ __launch_bounds__(64 * kRowWaves) void teacher_rows(Teacher teacher, int64_t tokens, int64_t *__restrict__ mark,
+                                                               Entry *__restrict__ entries, float *__restrict__ shares,
+                                                               uint16_t *__restrict__ strips, int64_t pitch)
+{
+    __shared__ RowShared<M> all[kRowWaves];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int64_t token = int64_t(blockIdx.x) * kRowWaves + wave;
+    if (token >= tokens) return;                         // (no barriers of blocks follow)
+    const TeacherRow r = row_entries<M, GRAD>(teacher, token, lane, all[wave], entries, shares, strips, pitch);
+    if (lane == 0) mark[token] = r.wrong ? kWrong : r.takes_part() ? kTakesPart : kNoPart;
+}
+
+// Few tokens of a gradient: their entries and all that the products need of them, in one launch instead of three (5 to 9 us each).  Nothing is listed:
+// a token that takes no part has a row of zeros and a factor of 0.  A block per row, zeros behind the last one up to whole tiles, once or (LOWER) twice;
+// the blocks behind them pad rows of the weight.
+constexpr int kFewRowWaves = 4;
+struct FewRows {
+    Header *header;          // of the tokens, and behind it of the products
+    int32_t *place;
+    float *base, *factor;
+    float outer;
+    int32_t top_bits;
+};
+template <typename T, int M, bool LOWER>
+__global__ __launch_bounds__(64 * kFewRowWaves) void few_rows(Teacher teacher, int64_t tokens, const float *__restrict__ lse, const float *__restrict__ dloss,
+                                                              const T *__restrict__ hidden, int64_t width, T *__restrict__ rows, int64_t pitch, FewRows out,
+                                                              Entry *__restrict__ entries, float *__restrict__ shares, Padding<T> weight)
+{
+    __shared__ RowShared<M> s;
+    __shared__ bool takes_part;
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t token = blockIdx.x, lower = lower_rows(tokens);
+    if (token >= lower) {
+        for (int64_t row = (token - lower) * kFewRowWaves + wave; row < weight.rows; row += (int64_t(gridDim.x) - lower) * kFewRowWaves)
+            copy_row(weight.src + row * weight.width, weight.width, weight.dst + row * weight.pitch, weight.pitch, lane, 64);
+        return;
+    }
+    if (wave == 0) {
+        TeacherRow r{0.f, 0.f, false};
+        if (token < tokens) r = row_entries<M, true>(teacher, token, lane, s, entries, shares, nullptr, 0);
+        float top = 0.f;                                 // (as list_tokens has it)
+        for (int64_t k = lane; k < tokens; k += 64) {
+            const float size = fabsf(dloss[k]);
+            if (size < __builtin_inff()) top = fmaxf(top, size);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+        const float unit = !out.top_bits || top == 0.f ? 1.f : fmaxf(top, 0x1p-100f), g = token < tokens ? dloss[token] : 0.f;
+        const bool part = token < tokens && r.takes_part() && g != 0.f;
+        if (lane == 0) {
+            takes_part = part;
+            if (token < tokens) {
+                out.place[token] = part ? int32_t(token) : -1;
+                out.base[token] = part ? lse[token] : 0.f;
+                out.factor[token] = !part ? 0.f : r.wrong ? __builtin_nanf("") : out.top_bits ? ldexpf(g / unit, out.top_bits - kLift) : g;
+            }
+            if (token == 0) {
+                const float unscale = ldexpf(unit, -out.top_bits) * out.outer;
+                out.header[0] = Header{int32_t(tokens), unscale};
+                if (LOWER) out.header[1] = Header{int32_t(2 * lower), unscale};
+            }
+        }
+    }
+    __syncthreads();
+    const T *const source = takes_part ? hidden + token * width : nullptr;
+    copy_row(source, width, rows + token * pitch, pitch, tid, 64 * kFewRowWaves);
+    if (LOWER) copy_row(source, width, rows + (lower + token) * pitch, pitch, tid, 64 * kFewRowWaves);
 }
 
 // A sum over the lanes of WAVES waves, in a fixed order; in the first of them.
@@ -271,19 +335,6 @@ __global__ __launch_bounds__(256) void delta_entries(const Header *header, Entri
     put_entry<T, T, LOWER>(entries, int64_t(blockIdx.x) * 256 + threadIdx.x, header, delta);
 }
 
-// The hidden states of d's two parts: the rows that count, in two sections with zeros behind them, and their header.  A block per row.
-template <typename T>
-__global__ __launch_bounds__(256) void split_rows(const Header *header, Hidden<T> hidden, T *__restrict__ rows, int64_t pitch, Header *both)
-{
-    const int64_t count = header->count, lower = lower_rows(count), row = blockIdx.x;
-    if (row == 0 && threadIdx.x == 0) *both = Header{int32_t(2 * lower), header->unscale};
-    if (row >= 2 * lower) return;
-    const int64_t from = row % lower;
-    const T *const source = hidden.of(count);
-    if (source == rows && row < count) return;           // (it is there already)
-    copy_row(from < count ? source + from * pitch : static_cast<const T *>(nullptr), pitch, rows + row * pitch, pitch, int(threadIdx.x), 256);
-}
-
 // bfloat16 to binary16, whose smaller range takes what is multiplied by a power of two, exactly: one that brings the largest magnitude into [2^14, 2^15).
 // Then everything down to 2^-31 of the largest keeps its eight bits.  The first pass converts with a guess of that power, and remembers the largest
 // magnitude its blocks saw; the second one converts again only where that did not come into [2^3, 2^15): down to 2^-20 of the largest all bits are kept then.
@@ -387,16 +438,16 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
     const HeadBuffers h = head_of(l, b);
     const Teacher teacher = teacher_of(l, b);
     Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
-    // Few tokens' kernel takes the products of the entries' rows along; tiles pick the logits out; the rest (17 to 64 tokens as they come, and so
-    // many entries that most columns are some) is gathered afterwards.
-    const bool direct = calls.direct(), few = calls.few(), tiles = !direct && l.tiles;
-    hipError_t error = direct ? hipSuccess : rows<false>(l, b, stream);
+    // Few tokens' kernel takes the products of the entries' rows along; tiles pick the logits out; where most columns are some token's entries, they are
+    // gathered afterwards.  (33 tokens x 2048 x 50257 bfloat16, 64 entries, picked 66 us, gathered 82.)
+    const bool direct = calls.direct(), few = calls.few(), tiles = !few && l.tiles;
+    hipError_t error = direct && !tiles ? hipSuccess : rows<false>(l, b, stream);
     if (few) {
         calls.picks.blocks = uint32_t((l.head.tokens * ((l.entries + kDots - 1) / kDots) + kFewWaves - 1) / kFewWaves);
         calls.picks.ids = b.ids;
         calls.picks.ignore = b.ignore;
     } else if (tiles) {
-        calls.tokens_of_rows = calls.template at<int32_t>(l.token);
+        calls.tokens_of_rows = calls.template at<int32_t>(l.token);       // (not written, nor read, where tokens are taken as they come)
         calls.picks.strips = calls.template at<uint16_t>(l.strip);
         calls.picks.entries = calls.template at<Entry>(l.entry);
         calls.picks.token = calls.tokens_of_rows;
@@ -413,7 +464,7 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
         join_picked<WAVES><<<dim3(uint32_t((l.head.tokens + kPerBlock - 1) / kPerBlock)), 64 * WAVES * kPerBlock, 0, stream>>>(
             teacher, l.head.tokens, place, parts, l.head.parts, stats, loss, lse, picked);
     };
-    if (few) join(std::integral_constant<int, kJoinWaves>());
+    if (few || (direct && tiles)) join(std::integral_constant<int, kJoinWaves>());
     else if (tiles) join(std::integral_constant<int, 1>());
     else
         join_gathered<T><<<dim3(uint32_t(l.head.tokens)), 64 * kGatherWaves, 0, stream>>>(
@@ -437,13 +488,30 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
         calls.weight_of_products = reinterpret_cast<D *>(at(l.weight16));
         calls.scales = reinterpret_cast<float *>(at(l.scales));
     }
-    hipError_t error = l.head.tokens ? rows<true>(l, b, stream) : hipSuccess;
+    hipError_t error = hipSuccess;
     const int64_t all = l.head.tokens * l.entries;
-    const auto listed = [&] {
-        if (!l.lower || !l.head.tokens) return;
-        split_rows<T><<<dim3(uint32_t(calls.product_rows())), 256, 0, stream>>>(calls.header(), calls.hidden(), calls.template at<T>(l.head.hidden), l.head.pitch,
-                                                                               calls.products());
+    const bool few = l.head.tokens > 0 && l.head.tokens <= kLowerTokens;
+    calls.copied = few;
+    const auto prepare_few = [&](auto most) {
+        constexpr int M = decltype(most)::value;
+        const int64_t columns = l.head.padded ? l.head.columns(0) : 0, wanted = (columns + kFewRowWaves - 1) / kFewRowWaves;
+        const int64_t pads = wanted < 8 * kHeadBlocks ? wanted : 8 * kHeadBlocks;
+        const FewRows out{calls.header(), calls.template at<int32_t>(l.head.place), calls.template at<float>(l.head.lse),
+                          calls.template at<float>(l.head.factor), inverse, calls.kTopBits};
+        few_rows<T, M, sizeof(T) == 2><<<dim3(uint32_t(lower_rows(l.head.tokens) + pads)), 64 * kFewRowWaves, 0, stream>>>(
+            teacher_of(l, b), l.head.tokens, lse, dloss, static_cast<const T *>(b.hidden), l.head.width, calls.template at<T>(l.head.hidden), l.head.pitch, out,
+            calls.template at<Entry>(l.entry), calls.template at<float>(l.share),
+            Padding<T>{static_cast<const T *>(b.weight), calls.template at<T>(l.head.weight), columns, l.head.width, l.head.pitch});
         calls.launched();
+    };
+    const auto listed = [&] {
+        if (!few) {
+            if (l.head.tokens) error = rows<true>(l, b, stream);
+            calls.list(dloss, lse, inverse);
+        } else if (l.entries <= 64) prepare_few(std::integral_constant<int, 64>());
+        else if (l.entries <= 128) prepare_few(std::integral_constant<int, 128>());
+        else if (l.entries <= 256) prepare_few(std::integral_constant<int, 256>());
+        else prepare_few(std::integral_constant<int, kMostEntries>());
     };
     const auto entries = [&](const T *w, int64_t first, int64_t columns) {
         const Entries n{calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
@@ -464,7 +532,7 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
             calls.launched();
         }
     };
-    const hipError_t rest = calls.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), inverse, listed, entries);
+    const hipError_t rest = calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), listed, entries);
     return error != hipSuccess ? error : rest;
 }
 

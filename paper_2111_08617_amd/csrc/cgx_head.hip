@@ -9,7 +9,8 @@ template <typename T>
 hipError_t gradient_of(const HeadLayout &l, const HeadBuffers &b, const float *lse, const float *dloss, void *dhidden, void *dweight,
                        hipStream_t stream)
 {
-    return Calls<T>{l, b, stream}.gradient(lse, dloss, static_cast<T *>(dhidden), static_cast<T *>(dweight), 1.f, [] {}, [](const T *, int64_t, int64_t) {});
+    const Calls<T> calls{l, b, stream};
+    return calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), [&] { calls.list(dloss, lse); }, [](const T *, int64_t, int64_t) {});
 }
 
 }  // namespace

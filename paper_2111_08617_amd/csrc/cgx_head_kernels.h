@@ -743,8 +743,8 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
 #pragma unroll
     for (int i = 0; i < K::TM; i++) {
         const int64_t row = m0 + tile.wm + 16 * i + r;
-        const bool counts = row < count;
-        const float base = counts ? lse[row] : 0.f, f = counts ? factor[row] : 0.f;
+        const float base = row < count ? lse[row] : 0.f, f = row < count ? factor[row] : 0.f;
+        const bool counts = row < count && (S::kTargets || f != 0.f);          // (few tokens are not listed: some may take no part)
         const int64_t hit = S::kTargets && counts ? int64_t(target[row]) - first - c0 : -1;
         D *const out = delta + row * piece + c0;
 #pragma unroll
@@ -756,7 +756,7 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
                 v[e] = D(d);
                 if (LOWER) rest[e] = D(d - float(v[e]));
             }
-            if (!whole)
+            if (!whole || (!S::kTargets && !counts))
 #pragma unroll
                 for (int e = 0; e < kPer; e++)
                     if (!counts || c0 + k + e >= columns) {
@@ -1040,6 +1040,7 @@ struct Calls {
     typename S::Picks picks = typename S::Picks();
     int32_t *tokens_of_rows = nullptr;
     bool lower = false;
+    bool copied = false;                                                   // hidden states are read from their copies, whichever tokens count
     D *hidden_of_products = nullptr, *weight_of_products = nullptr;        // where D is another type
     float *scales = nullptr;                                               // of the hidden states, of the weight's piece: 1 / the power of two
     static constexpr bool kOther = !std::is_same<D, T>::value;
@@ -1063,7 +1064,7 @@ struct Calls {
     Hidden<T> hidden() const
     {
         // (whole steps of tokens: the gradient's products sum over them)
-        const bool fits = !l.padded && l.tokens % head_depth(l.dt) == 0;
+        const bool fits = !copied && !l.padded && l.tokens % head_depth(l.dt) == 0;
         return Hidden<T>{fits ? static_cast<const T *>(b.hidden) : nullptr, at<T>(l.hidden), l.tokens};
     }
     // The list, and the first piece of the weight in padded rows where they have to be.
@@ -1074,8 +1075,7 @@ struct Calls {
         const int64_t columns = l.padded && l.tokens ? l.columns(0) : 0, wanted = (columns + kListThreads / 64 - 1) / (kListThreads / 64);
         const int64_t pads = wanted < 8 * kHeadBlocks ? wanted : 8 * kHeadBlocks;
         list_tokens<T><<<dim3(uint32_t(grid + pads)), kListThreads, 0, stream>>>(
-            b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, std::is_same<D, _Float16>::value ? 14 : std::is_same<D, __bf16>::value ? kLift : 0,
-            outer, static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, int32_t(head_depth(l.dt)), h.own ? 1 : 0, header(),
+            b.targets, dloss, lse, l.tokens, b.ignore, l.vocab, kTopBits, outer, static_cast<const T *>(b.hidden), l.width, at<T>(l.hidden), l.pitch, int32_t(head_depth(l.dt)), h.own ? 1 : 0, header(),
             Lists{at<int32_t>(l.place), at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), tokens_of_rows}, uint32_t(grid),
             Padding<T>{static_cast<const T *>(b.weight), at<T>(l.weight), columns, l.width, l.pitch});
         launched();
@@ -1239,12 +1239,12 @@ struct Calls {
                                                                                         dweight + first * l.width, at<float>(l.spare), scales);
         launched();
     }
-    // listed(): queues what the products' hidden states need once the tokens are listed; entries(w, first, columns): what d of a piece lacks, and what the
+    static constexpr int kTopBits = std::is_same<D, _Float16>::value ? 14 : std::is_same<D, __bf16>::value ? kLift : 0;
+    // listed(): queues the list of tokens and what the products' hidden states need; entries(w, first, columns): what d of a piece lacks, and what the
     // products' weights need.
     template <class Listed, class Entries>
-    hipError_t gradient(const float *lse, const float *dloss, T *dhidden, T *dweight, float outer, Listed listed, Entries entries) const
+    hipError_t gradient(T *dhidden, T *dweight, Listed listed, Entries entries) const
     {
-        list(dloss, lse, outer);
         listed();
         const Size sums = sums_size();
         for (int64_t k = 0; k < l.pieces; k++) {
