@@ -28,7 +28,9 @@ struct DistillLayout {
 };
 
 constexpr int kConvertBlocks = 1024;
-constexpr int64_t kLowerTokens = 128;                // up to this many tokens take d in two parts: rows for both are there
+// Up to this many tokens of a gradient are not listed, and hold a 16-bit d in two parts: rows for both are there.  us with two parts and, for bfloat16 in
+// binary16, for binary16 in one: 128 x 2048 x 50257 326 and 403, 330 and 326; 256 x 2048 x 50257 458 and 438, 465 and 340.
+constexpr int64_t kLowerTokens = 128;
 
 // CGX_OK and the layout, or the error of the sizes.
 int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries, int dt, bool grad, DistillLayout *out);
