@@ -3,8 +3,9 @@
     python examples/train_step.py [steps]
 
 The model predicts the next token from the current one: an embedding, a mixing matrix and a head over the vocabulary.  PyTorch
-differentiates the two layers in front; everything from the hidden states on runs in this library's kernels:
+differentiates the matrix between them; the embedding and everything from the hidden states on run in this library's kernels:
 
+  cgx_embed, cgx_embed_grad           the tokens' rows of the embedding, and the embedding's gradient from theirs
   cgx_head_loss, cgx_head_loss_grad   the loss over the vocabulary and its gradients, without the logits
   cgx_grad_clip                       (with no limit yet) the gradients of all layers, converted into one fused buffer
   cgx_quantize                        that buffer, compressed layer by layer: what the rank would send
@@ -46,24 +47,29 @@ class Model:
         packed_bytes, meta_bytes = cgx.cgx_sizes(self.plan)
         self.packed = torch.empty(packed_bytes, dtype=torch.uint8, device="cuda")
         self.meta = torch.empty(meta_bytes // 4, device="cuda")
-        # what the head and the norm need, kept over the steps
+        # what the head, the embedding and the norm need, kept over the steps
         self.workspace = torch.empty(cgx.cgx_head_workspace(BATCH, WIDTH, VOCAB, cgx.BF16, grad=True), dtype=torch.uint8, device="cuda")
+        self.embed_workspace = torch.empty(cgx.cgx_embed_grad_workspace(BATCH, WIDTH, VOCAB, cgx.F32), dtype=torch.uint8, device="cuda")
         self.norm_workspace = torch.empty(cgx.cgx_grad_norm_workspace(), dtype=torch.uint8, device="cuda")
         self.loss, self.lse = torch.empty(BATCH, device="cuda"), torch.empty(BATCH, device="cuda")
         self.norm, self.zero = torch.empty(1, device="cuda"), torch.zeros(1, device="cuda")
 
     def gradients(self, tokens, targets):
         """(mean loss, gradients of the layers) of one batch; targets may hold IGNORE."""
-        hidden = torch.tanh(self.embedding[tokens] @ self.mix).to(torch.bfloat16)
+        rows = torch.empty(BATCH, WIDTH, device="cuda")
+        cgx.cgx_embed(self.embedding.detach(), tokens, rows)
+        hidden = torch.tanh(rows.requires_grad_() @ self.mix).to(torch.bfloat16)
         head = self.head.to(torch.bfloat16)
         cgx.cgx_head_loss(hidden.detach(), head, targets, self.loss, self.lse, self.workspace, ignore=IGNORE)
         counted = (targets != IGNORE).sum().clamp(min=1)
         dloss = (1.0 / counted).expand(BATCH).contiguous()
         dhidden, dhead = torch.empty_like(hidden), torch.empty_like(head)
         cgx.cgx_head_loss_grad(hidden.detach(), head, targets, self.lse, dloss, dhidden, dhead, self.workspace, ignore=IGNORE)
-        self.embedding.grad = self.mix.grad = None
+        self.mix.grad = None
         hidden.backward(dhidden)
-        return self.loss.sum() / counted, [self.embedding.grad, self.mix.grad, dhead]
+        dembedding = torch.empty_like(self.embedding, requires_grad=False)
+        cgx.cgx_embed_grad(rows.grad, tokens, dembedding, self.embed_workspace)
+        return self.loss.sum() / counted, [dembedding, self.mix.grad, dhead]
 
     def step(self, tokens, targets, seed: int, rate: float = 2.0, max_norm: float = 1.0):
         loss, grads = self.gradients(tokens, targets)

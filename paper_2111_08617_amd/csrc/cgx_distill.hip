@@ -317,10 +317,10 @@ template <typename T, typename D, bool LOWER>
 __device__ __forceinline__ void put_entry(const Entries &n, int64_t k, const Header *header, D *__restrict__ delta)
 {
     if (k >= n.all) return;
-    const int64_t token = k / n.count;
+    const int64_t token = uint32_t(k) / uint32_t(n.count);       // (fewer than 2^31 entries)
     const int32_t row = n.place[token];
-    if (row < 0) return;                                 // (it may have no sorted entries)
     const Entry e = n.entries[k];
+    if (row < 0) return;                                 // (it may have no sorted entries)
     const int64_t column = e.id - n.from;
     if (e.id < 0 || column < 0 || column >= n.columns) return;
     const float z = n.picked[token * n.count + e.place];

@@ -105,3 +105,21 @@ def test_binding_refuses_what_the_kernels_would_overrun(lib):
         with pytest.raises(cgx.CgxError) as e:
             cgx.cgx_embed_grad_workspace(*sizes, cgx.F32)
         assert e.value.status == SIZE
+
+
+def test_workspaces_are_clean_under_asan_and_ubsan(tmp_path):
+    """The host code that lays out the workspaces of these calls and of distillation, on many sizes."""
+    import shutil
+    import subprocess
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    here = os.path.dirname(os.path.abspath(__file__))
+    csrc = os.path.join(os.path.dirname(here), "paper_2111_08617_amd", "csrc")
+    exe = str(tmp_path / "driver")
+    subprocess.run(["g++", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-g", "-O1", "-std=c++17",
+                    os.path.join(here, "host_sanitize", "more_layouts.cpp"),
+                    *(os.path.join(csrc, f) for f in ("cgx_embed.cpp", "cgx_distill.cpp", "cgx_head.cpp")), "-o", exe], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "all checks passed" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
+    taken, refused = (int(w) for w in run.stdout.split() if w.isdigit())
+    assert taken > 5000 and refused > 5000
