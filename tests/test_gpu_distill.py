@@ -154,7 +154,7 @@ def test_divergence_and_gradients(torch, shape, dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("shape", [(512, 64, 25000, 64), (6150, 2048, 300, 20), (70, 2040, 6200, 256), (1, 2048, 50257, 64), (33, 768, 30522, 32),
-                                   (100, 1024, 20000, 1000), (3000, 64, 5000, 128)], ids=lambda s: "x".join(map(str, s)))
+                                   (100, 1024, 20000, 1000), (3000, 64, 5000, 128), (40, 64, 8000, 1000)], ids=lambda s: "x".join(map(str, s)))
 def test_sizes_that_fill_the_chip(torch, shape, dtype):
     check(torch, *inputs(torch, *shape, dtype, seed=3), torch.full((shape[0],), 1.0 / shape[0], device="cuda"), temperature=1.5)
 
@@ -386,3 +386,15 @@ def test_operands_with_outliers_in_bfloat16(torch):
     weight[:, 7] *= 2.0**-20
     weight[5, 9] = 24.0
     check(torch, hidden, weight, ids, teacher, torch.full((300,), 0.5, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens", [40, 150])
+def test_most_entries_in_a_few_columns(torch, tokens):
+    """More than 63 in 64 columns: once, twice, at both ends of the vocabulary."""
+    hidden, weight, ids, teacher = inputs(torch, tokens, 128, 20000, 1000, "bf16", seed=2, marked=0.0)
+    ids[::3] = torch.arange(1000, device="cuda") % 100
+    ids[1::3] = 19999 - torch.arange(1000, device="cuda") % 64
+    ids[2::3, 100:163] = 320 + torch.arange(63, device="cuda")
+    ids[5, 100:164] = 320 + torch.arange(64, device="cuda")
+    ids[8] = 64
+    check(torch, hidden, weight, ids, teacher, torch.full((tokens,), 0.1, device="cuda"))

@@ -332,3 +332,25 @@ def test_many_tokens_with_padding_and_ids_outside(torch, vocab):
     dout[ids == -100] = 0.5
     dout[ids == 1] = float("nan")
     gradient(torch, dout, ids, vocab, ignore=1)                # an entry of the vocabulary as padding
+
+
+@pytest.mark.parametrize("tokens", [5, 300])
+def test_the_longest_vocabulary(torch, tokens):
+    """2^28 - 1 entries of one element: launches stay within their bounds, and every element is written."""
+    vocab = (1 << 28) - 1
+    g = torch.Generator().manual_seed(1)
+    ids = torch.randint(0, vocab, (tokens,), generator=g).cuda()
+    ids[0], ids[1], ids[2] = 0, vocab - 1, (1 << 27) + 1
+    dout = torch.randint(1, 9, (tokens, 1), generator=g).bfloat16().cuda()
+    dtable = torch.full((vocab, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(cgx.cgx_embed_grad_workspace(tokens, 1, vocab, cgx.BF16), dtype=torch.uint8, device="cuda")
+    cgx.cgx_embed_grad(dout, ids, dtable, ws)
+    want = {}
+    for k, v in zip(ids.tolist(), dout[:, 0].tolist()):
+        want[k] = want.get(k, 0.0) + v
+    at = torch.nonzero(dtable[:, 0])[:, 0]
+    assert at.tolist() == sorted(want)
+    assert dtable[at, 0].tolist() == [want[k] for k in sorted(want)]          # (whole numbers of at most 8 bits)
+    out = torch.empty(tokens, 1, dtype=torch.bfloat16, device="cuda")
+    cgx.cgx_embed(dtable, ids, out)
+    assert out[:, 0].tolist() == [want[k] for k in ids.tolist()]
