@@ -712,11 +712,23 @@ def cgx_head_loss_grad(hidden, weight, targets, lse, dloss, dhidden, dweight, wo
 def _here(name: str, stream, *tensors) -> int:
     """The stream of a call, which runs on the current device: tensors of another one are refused."""
     import torch
-    device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
     for t, what in tensors:
         if t.get_device() != device:
             raise ValueError(f"{name}: {what}: the tensor lives on {t.device}, the call runs on the current device, cuda:{device}")
+    if stream is None and torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(device)
     return _stream(stream)
+
+
+_types = {}
+
+
+def _type_of(dtype):
+    """The number of an element type (None: not one of these), looked up by the object after its first time: its name costs a third of a microsecond."""
+    if dtype not in _types:
+        _types[dtype] = _HEAD_TYPES.get(str(dtype))
+    return _types[dtype]
 
 
 def cgx_head_distill_workspace(tokens: int, width: int, vocab: int, entries: int, dt: int, grad: bool = False) -> int:
@@ -733,7 +745,7 @@ def _distill(name: str, hidden, weight, ids, teacher, ignore: int, temperature: 
         if getattr(t, "ndim", 0) != 2:
             raise ValueError(f"{name}: {what}: a matrix is needed, a row for each {rows}")
     (tokens, width), (vocab, across), (rows, entries) = hidden.shape, weight.shape, ids.shape
-    dt, teacher_dt = _HEAD_TYPES.get(str(hidden.dtype)), _HEAD_TYPES.get(str(teacher.dtype))
+    dt, teacher_dt = _type_of(hidden.dtype), _type_of(teacher.dtype)
     for t, what, known in ((hidden, "hidden", dt), (teacher, "teacher", teacher_dt)):
         if known is None:
             raise ValueError(f"{name}: {what}: element type {t.dtype}, expected torch.float32, torch.float16 or torch.bfloat16")
@@ -792,7 +804,7 @@ def _embedding(name: str, table, what: str, ids, rows, across: str):
         if getattr(t, "ndim", 0) != 2:
             raise ValueError(f"{name}: {w}: a matrix is needed, a row for each {'entry of the vocabulary' if t is table else 'token'}")
     (vocab, width), (tokens, wide) = table.shape, rows.shape
-    dt = _HEAD_TYPES.get(str(table.dtype))
+    dt = _type_of(table.dtype)
     if dt is None:
         raise ValueError(f"{name}: {what}: element type {table.dtype}, expected torch.float32, torch.float16 or torch.bfloat16")
     if wide != width:
