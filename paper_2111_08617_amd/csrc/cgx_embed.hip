@@ -597,7 +597,8 @@ hipError_t gradient(const EmbedLayout &l, const void *dout, const int64_t *ids, 
 {
     Launches g{stream};
     if (l.tokens && l.tokens <= kFewTokens) {
-        const int64_t each = l.vocab < int64_t(1) << 26 ? 4 : 16;       // (a launch has fewer than 2^32 threads)
+        // (one row a wave while the chip holds twice as many waves; a launch has fewer than 2^32 threads)
+        const int64_t each = l.vocab * l.strips <= 16384 ? 1 : l.vocab < int64_t(1) << 26 ? 4 : 16;
         const int64_t items = (accumulate ? l.tokens : (l.vocab + each - 1) / each) * l.strips;
         few_rows<T><<<dim3(uint32_t((items + kBlock / 64 - 1) / (kBlock / 64))), kBlock, 0, stream>>>(
             ids, static_cast<const T *>(dout), int32_t(l.tokens), ignore, l.vocab, l.width, uint32_t(l.strips), scale, accumulate,
