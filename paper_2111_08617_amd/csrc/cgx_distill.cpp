@@ -10,8 +10,6 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     if (rc != CGX_OK) return rc;
     if (entries < 1 || entries > kMostEntries || tokens * entries >= int64_t(1) << 31) return CGX_ERR_SIZE;
     l.entries = entries;
-    // (with more entries than this in every 64 columns a tile's end would take longer than the tile)
-    l.tiles = int64_t(entries) * 64 <= 4 * vocab;
     l.strips = (vocab + 511) / 512 * 8;
     size_t at = l.head.bytes;
     const auto take = [&at](int64_t bytes) {
@@ -22,13 +20,10 @@ int distill_layout(int64_t tokens, int64_t width, int64_t vocab, int32_t entries
     l.mark = take(tokens * 8);
     l.token = take(tokens * 4);
     l.entry = take(tokens * entries * 8 + 16);           // (they are read in pairs)
-    // the shares are the gradient call's, the strips the loss's
+    // the strips are the loss's, what follows the gradient call's; a workspace for that is one for both
     const size_t shared = at;
+    l.strip = take(tokens * l.strips * 2);
     size_t end = at;
-    if (l.tiles) {
-        l.strip = take(tokens * l.strips * 2);
-        end = at;
-    }
     if (grad) {
         at = shared;
         l.share = take(tokens * entries * 4);

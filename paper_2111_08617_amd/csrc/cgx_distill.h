@@ -11,13 +11,12 @@ constexpr int kMostEntries = 1024;                   // of the teacher, a token
 struct DistillLayout {
     HeadLayout head;
     int32_t entries = 0;
-    bool tiles = false;      // the loss picks the student's logits out of the tiles they are formed in
     int64_t strips = 0;      // of 64 columns of the vocabulary, rounded up to a multiple of 8
     size_t mark = 0;         // int64 [tokens]: what the head's list reads as targets: kTakesPart, kNoPart or (kWrong) not a number
     size_t token = 0;        // int32 [tokens]: of a row of the list
     size_t entry = 0;        // Entry [tokens][entries]: sorted by id; those that are none are the last, with an id of -1
     size_t share = 0;        // float [tokens][entries] (gradient): of the entries in that order; ids that come again have theirs added to the first
-    size_t strip = 0;        // uint16 [tokens][strips] (loss, tiles): see Picks
+    size_t strip = 0;        // uint16 [tokens][strips] (loss): see Picks
     bool lower = false;      // (gradient) d is held in two parts, see Calls
     bool other = false;      // (gradient) d, and the operands of its products, are held in binary16 instead of bfloat16
     size_t most = 0;         // float [2][kConvertBlocks]: the largest magnitudes that the blocks of a conversion have seen

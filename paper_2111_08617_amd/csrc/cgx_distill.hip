@@ -268,40 +268,6 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_picked(T
     loss[token] = !takes_part ? 0.f : row.wrong ? __builtin_nanf("") : sum;
 }
 
-// The same where no logits were picked: a block per token takes the products of its entries' rows, a wave kDots of them.
-constexpr int kGatherWaves = 4;
-template <typename T>
-__global__ __launch_bounds__(64 * kGatherWaves) void join_gathered(Teacher teacher, const int32_t *__restrict__ place, int64_t parts, int64_t pitch,
-                                                                   const float2 *__restrict__ stats, const T *__restrict__ hidden,
-                                                                   const T *__restrict__ weight, int64_t width, float *__restrict__ loss,
-                                                                   float *__restrict__ lse, float *__restrict__ picked)
-{
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t token = blockIdx.x, first = token * teacher.entries;
-    const TeacherRow row = teacher_row(teacher, token, lane);
-    if (!row.takes_part()) {                             // (the same in all waves)
-        for (int k = tid; k < teacher.entries; k += 64 * kGatherWaves) picked[first + k] = 0.f;
-        if (tid == 0) loss[token] = lse[token] = 0.f;
-        return;
-    }
-    const float total = log_sum<kGatherWaves>(stats + (place ? int64_t(place[token]) : token) * pitch, parts, tid);
-    const float log_mass = row.top + logf(row.sum);
-    float sum = 0.f;
-    for (int k0 = wave * kDots; k0 < teacher.entries; k0 += kGatherWaves * kDots)
-        entry_dots(hidden + token * width, weight, width, teacher.vocab, teacher.ids + first, teacher.ignore, k0, teacher.entries, lane,
-                   [&](int k, int64_t id, bool inside, float z) {
-                       if (lane != 0) return;
-                       picked[first + k] = id == teacher.ignore ? 0.f : inside ? z : __builtin_nanf("");
-                       if (id == teacher.ignore) return;
-                       const float scaled = teacher.logit(first + k) * teacher.inverse, q = row.share(scaled);
-                       if (q > 0.f) sum += q * (scaled - log_mass + total - z * teacher.inverse);
-                   });
-    sum = lanes_sum<kGatherWaves>(sum, tid);
-    if (tid != 0) return;
-    lse[token] = total;
-    loss[token] = row.wrong ? __builtin_nanf("") : sum;
-}
-
 // d at the teacher's entries within a piece of the vocabulary, in its units: a thread per entry.
 struct Entries {
     const Entry *entries;
@@ -418,7 +384,7 @@ hipError_t rows(const DistillLayout &l, const DistillBuffers &b, hipStream_t str
         teacher_rows<M, GRAD><<<dim3(uint32_t((l.head.tokens + kRowWaves - 1) / kRowWaves)), 64 * kRowWaves, 0, stream>>>(
             teacher_of(l, b), l.head.tokens, reinterpret_cast<int64_t *>(b.workspace + l.mark), reinterpret_cast<Entry *>(b.workspace + l.entry),
             GRAD ? reinterpret_cast<float *>(b.workspace + l.share) : nullptr,
-            !GRAD && l.tiles ? reinterpret_cast<uint16_t *>(b.workspace + l.strip) : nullptr, l.strips);
+            !GRAD ? reinterpret_cast<uint16_t *>(b.workspace + l.strip) : nullptr, l.strips);
     };
     if (l.entries <= 64) go(std::integral_constant<int, 64>());
     else if (l.entries <= 128) go(std::integral_constant<int, 128>());
@@ -438,15 +404,16 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
     const HeadBuffers h = head_of(l, b);
     const Teacher teacher = teacher_of(l, b);
     Calls<T, Tempered> calls{l.head, h, stream, Tempered{teacher.inverse}};
-    // Few tokens' kernel takes the products of the entries' rows along; tiles pick the logits out; where most columns are some token's entries, they are
-    // gathered afterwards.  (33 tokens x 2048 x 50257 bfloat16, 64 entries, picked 66 us, gathered 82.)
-    const bool direct = calls.direct(), few = calls.few(), tiles = !few && l.tiles;
-    hipError_t error = direct && !tiles ? hipSuccess : rows<false>(l, b, stream);
+    // Few tokens' kernel takes the products of the entries' rows along; other tiles pick the logits out.  Both against products of gathered rows after the
+    // tiles, us: one token x 1024 x 50257 binary16 24.7 and 30.7; picked 33 x 2048 x 50257 bfloat16, 64 entries, 57 and 82, 2048 x 2048 x 50257 384 and 461,
+    // 2000 x 512 x 1000 of 16, 64 and 256 entries 29, 35, 66 and 36, 57, 144, 2000 x 2048 x 5000 of 1000 entries 282 and 1384.
+    const bool direct = calls.direct(), few = calls.few();
+    hipError_t error = few ? hipSuccess : rows<false>(l, b, stream);
     if (few) {
         calls.picks.blocks = uint32_t((l.head.tokens * ((l.entries + kDots - 1) / kDots) + kFewWaves - 1) / kFewWaves);
         calls.picks.ids = b.ids;
         calls.picks.ignore = b.ignore;
-    } else if (tiles) {
+    } else {
         calls.tokens_of_rows = calls.template at<int32_t>(l.token);       // (not written, nor read, where tokens are taken as they come)
         calls.picks.strips = calls.template at<uint16_t>(l.strip);
         calls.picks.entries = calls.template at<Entry>(l.entry);
@@ -464,11 +431,8 @@ hipError_t divergence(const DistillLayout &l, const DistillBuffers &b, float *lo
         join_picked<WAVES><<<dim3(uint32_t((l.head.tokens + kPerBlock - 1) / kPerBlock)), 64 * WAVES * kPerBlock, 0, stream>>>(
             teacher, l.head.tokens, place, parts, l.head.parts, stats, loss, lse, picked);
     };
-    if (few || (direct && tiles)) join(std::integral_constant<int, kJoinWaves>());
-    else if (tiles) join(std::integral_constant<int, 1>());
-    else
-        join_gathered<T><<<dim3(uint32_t(l.head.tokens)), 64 * kGatherWaves, 0, stream>>>(
-            teacher, place, parts, l.head.parts, stats, static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight), l.head.width, loss, lse, picked);
+    if (direct) join(std::integral_constant<int, kJoinWaves>());
+    else join(std::integral_constant<int, 1>());
     calls.launched();
     if (error == hipSuccess) error = calls.error;
     return error;

@@ -10,7 +10,7 @@ namespace cgx {
 
 constexpr int kEmbedSortBlocks = 256;                // compute units: each sorts the tokens of its share of the vocabulary
 constexpr int kEmbedParts = 256;                     // that many tokens are cut into before they are sorted: a block each
-constexpr int64_t kEmbedManyTokens = 16384;          // from which on
+constexpr int64_t kEmbedManyTokens = 24576;          // from which on
 constexpr int kEmbedMostChunk = 64;                  // sorted tokens that a wave sums at most: a lane holds each of them
 
 struct SortedToken {

@@ -66,7 +66,7 @@ static bool distill(int64_t n, int64_t h, int64_t v, int32_t k, int dt, bool gra
     if (!fits) return false;
     CHECK(l.head.bytes == head.bytes && l.entries == k && l.strips % 8 == 0 && l.strips * 64 >= v);
     Sections s{{l.mark, n * 8}, {l.token, n * 4}, {l.entry, n * k * 8 + 16}};
-    if (!grad && l.tiles) s.push_back({l.strip, n * l.strips * 2});
+    if (!grad) s.push_back({l.strip, n * l.strips * 2});
     if (grad) s.push_back({l.share, n * k * 4});
     if (l.lower) {
         // two parts of d, and the hidden states twice, in the rows that are there
@@ -81,6 +81,8 @@ static bool distill(int64_t n, int64_t h, int64_t v, int32_t k, int dt, bool gra
         s.push_back({l.weight16, l.head.piece * l.head.pitch * 2});
     }
     disjoint(s, l.bytes, l.head.bytes);
+    DistillLayout loss;
+    CHECK(distill_layout(n, h, v, k, dt, false, &loss) == CGX_OK && loss.bytes <= l.bytes);      // (for both calls)
     return true;
 }
 
