@@ -284,6 +284,8 @@ using Lds = unsigned char[K::kLds];
 // Picks a tile's logits at its rows' entries.  Most rows have no entry among a wave's 64 columns, or one, anywhere, and registers have no index: so
 // a wave that has any puts its logits into LDS, as many rows as its share of that holds, and each lane looks up one row's.  The loads that depend on each
 // other are spread over the tile's end: where a row's entries are when it begins, the first two of them half way through the exponentials.
+// Tiles with and without picking, us: 8192 x 2048 x 50257 bfloat16, 64 entries, 1292 and 1257; 4096 x 1024 x 50257 binary16, 128, 415 and 383; 615 x 768 x
+// 30522, 32, 51 and 47.  Picking from the registers, by comparing each of a lane's sixteen columns: 1350, 449 and 56.
 template <typename K, typename S>
 struct Picker {
     __device__ __forceinline__ Picker(const typename S::Picks &, const K &, const Tokens &, int64_t, int64_t, int64_t) {}
