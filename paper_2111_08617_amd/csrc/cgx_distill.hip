@@ -137,8 +137,10 @@ __device__ __forceinline__ TeacherRow row_entries(const Teacher &teacher, int64_
         entries[first + k] = e;
     }
     if (GRAD || !strips) return r;
+    // The first entry of a strip writes it, once the zeros have arrived.
     wave_fence();
-    // The first entry of a strip writes it, after the zeros: stores of a wave to one address are in order
+    __builtin_amdgcn_s_waitcnt(0x0f70);                  // (no access to memory is on its way)
+    wave_fence();
     const auto strip_of = [](uint64_t key) { return int64_t(key >> kStripBits) / kStripColumns; };
     for (int k = lane; k < teacher.entries; k += 64) {
         const uint64_t key = s.key[k];
@@ -237,8 +239,8 @@ __device__ __forceinline__ float lanes_sum(float v, int lane)
     return v;
 }
 
-// The loss from the parts of a token's softmax and its picked logits (8192 tokens of 197 parts and 64 entries 10 us; one token 5): a wave per token, four of them in a block, or (few tokens) a block of many waves
-// per token.
+// The loss from the parts of a token's softmax and its picked logits: a wave per token, four of them in a block, or (few tokens) a block of many waves
+// per token.  8192 tokens of 197 parts and 64 entries 10 us; one token 5.
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_picked(Teacher teacher, int64_t tokens, const int32_t *__restrict__ place,
                                                                                int64_t parts, int64_t pitch, const float2 *__restrict__ stats,
@@ -328,9 +330,8 @@ __device__ __forceinline__ float block_most(float v)
 // rows.to may be null: the hidden states are converted with the first piece of the weight.  The second pass' blocks behind the first kConvertBlocks see to
 // the teacher's entries.
 template <bool AGAIN>
-__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, const __bf16 *__restrict__ source_weight, Conversion rows,
-                                                    Conversion weight,
-                                                    Entries entries, _Float16 *__restrict__ delta)
+__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, const __bf16 *__restrict__ source_weight,
+                                                    Conversion rows, Conversion weight, Entries entries, _Float16 *__restrict__ delta)
 {
     if (AGAIN && blockIdx.x >= kConvertBlocks) {
         put_entry<__bf16, _Float16, false>(entries, int64_t(blockIdx.x - kConvertBlocks) * 256 + threadIdx.x, header, delta);

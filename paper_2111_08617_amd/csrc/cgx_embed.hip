@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__res
         token = e.token;
         return exists;
     };
-    // A sum over the block, in every thread; `own` is thread 0's.
+    // What is ahead of the share, a sum over the block, and how many tokens it has (thread 0 says), in every thread.
     const auto totals = [&](uint32_t ahead, uint32_t count) {
         const uint32_t x = wave_sum(ahead);
         if ((tid & 63) == 0) s.ahead[tid >> 6] = x;
