@@ -459,7 +459,8 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  * d is held more exactly here, since the entries' elements are not near 1 as a target's is: in two parts for up to 128 tokens, and in binary16 for
  * more tokens of bfloat16, whose operands then are converted as well: an element of d below 2^-28 of the largest dloss loses bits, one below 2^-39 is
  * lost, and so are bits of operands below 2^-20 of the largest one.
- * 1 <= entries <= 1024 (more than vocab are allowed), tokens x entries < 2^31, 2^-64 <= temperature <= 2^64 (CGX_ERR_SIZE otherwise).
+ * 1 <= entries <= 1024 (more than vocab are allowed), tokens x entries < 2^31, 2^-10 <= temperature <= 2^10 (CGX_ERR_SIZE otherwise).
+ * Logits over the temperature are formed in binary32, and a probability is off by some 2^-22 of the token's |lse|, as it is above.
  */
 int cgx_head_distill_workspace(int64_t tokens, int32_t width, int64_t vocab, int32_t entries, cgx_dtype dt,
                                int32_t grad /* 0: for cgx_head_distill; else for both calls */, size_t *bytes);

@@ -37,7 +37,7 @@ int check_distill(int64_t tokens, int32_t width, int64_t vocab, int32_t entries,
     const int rc = cgx::distill_layout(tokens, width, vocab, entries, dt, grad, l);
     if (rc != CGX_OK) return rc;
     if (!known_type(teacher_dt)) return CGX_ERR_DTYPE;
-    return temperature >= 0x1p-64f && temperature <= 0x1p64f ? CGX_OK : CGX_ERR_SIZE;
+    return temperature >= 0x1p-10f && temperature <= 0x1p10f ? CGX_OK : CGX_ERR_SIZE;
 }
 
 }  // namespace

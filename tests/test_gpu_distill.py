@@ -6,7 +6,7 @@ Tolerances follow from the arithmetic.  With u the unit roundoff of the operands
   most 100 terms in a row (100 * 2^-24), together under 1.2e-5; and the rounding of the result, 2^-23 |lse|
   q: relative, exp of a difference (2^-23 and 2^-23 of the magnitudes in it) and a sum of at most 1024 terms in 64 lanes (22 * 2^-24)
   loss: those of q, of lse and of picked in its terms, the terms' own roundings (2^-22 of the magnitudes in them), sums of `entries` terms
-  d: relative 2 (e / T + 2^-23 |z| / T) + 1.2e-5 + 2^-23 |lse| of its probability, q's error, 2^-23 of both for the difference, and u of
+  d: relative (e / T + 2^-23 |z| / T, of the logit and of the row's largest) + 1.2e-5 + 2^-23 |lse| of its probability, q's error, 2^-23 of both for the difference, and u of
   itself where it is rounded to the operands' type or a finer one (binary16, which also holds that of many bfloat16 tokens: at least half a
   subnormal step under the scale, 2^-39 of the largest factor)
   operands in binary16 instead of bfloat16: half a subnormal step under their power of two, 2^-25 / 2^3 of the largest magnitude
@@ -129,7 +129,9 @@ def check(torch, hidden, weight, ids, teacher, dloss=None, temperature=1.0, igno
     x = torch.where(kept, x, 0.0)
     smallest = 2.0**-39 * float(dloss.abs().max()) if name != "f32" and len(dloss) else 0.0
     step = 2.0**-28 if name == "bf16" else 0.0
-    off = g.abs() * (p * (2 * off_z + 1.2e-5 + 2.0**-22 * (1 + lse.abs())) + off_entries + 2.0**-23 * (p + at_entries)) * 1.01 + u * d.abs() + smallest
+    # (a logit's own error, and that of lse, which is the largest logit's at most)
+    of_p = off_z + (off_z.max(dim=1, keepdim=True).values if len(rows) else off_z[:, :1])
+    off = g.abs() * (p * (of_p + 1.2e-5 + 2.0**-22 * (1 + lse.abs())) + off_entries + 2.0**-23 * (p + at_entries)) * 1.01 + u * d.abs() + smallest
     off = torch.where(kept, off, 0.0)
     least = 2.0**-25 if name == "f16" else 1e-38
     dx, dw = torch.mm(d, w) / t, torch.mm(d.t().contiguous(), x) / t
@@ -169,7 +171,7 @@ def test_a_vocabulary_in_several_pieces(torch, dtype):
     check(torch, *args, torch.full((tokens,), 0.25, device="cuda"))
 
 
-@pytest.mark.parametrize("temperature", [0.25, 1.0, 8.0, 100.0])
+@pytest.mark.parametrize("temperature", [2.0**-10, 0.25, 1.0, 8.0, 100.0, 2.0**10])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_temperatures(torch, dtype, temperature):
     check(torch, *inputs(torch, 90, 64, 700, 30, dtype, seed=2), torch.linspace(-1, 1, 90, device="cuda"), temperature=temperature)
@@ -398,3 +400,35 @@ def test_most_entries_in_a_few_columns(torch, tokens):
     ids[5, 100:164] = 320 + torch.arange(64, device="cuda")
     ids[8] = 64
     check(torch, hidden, weight, ids, teacher, torch.full((tokens,), 0.1, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens", [3, 70, 140])
+def test_the_widest_hidden_states(torch, tokens):
+    check(torch, *inputs(torch, tokens, 1 << 17, 40, 8, "bf16", seed=1), torch.full((tokens,), 0.1, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens", [10, 150])
+def test_an_entry_of_the_vocabulary_as_the_mark(torch, tokens):
+    hidden, weight, ids, teacher = inputs(torch, tokens, 64, 50, 9, "f16", seed=1, marked=0.0)
+    ids[4] = 7
+    got = check(torch, hidden, weight, ids, teacher, torch.full((tokens,), 0.1, device="cuda"), ignore=7)
+    assert got["loss"][4] == 0 and (got["dhidden"][4] == 0).all()
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own(torch):
+    tokens, width, vocab, entries = 600, 256, 4000, 32
+    args = [inputs(torch, tokens, width, vocab, entries, "bf16", seed=k) for k in range(2)]
+    dloss = torch.full((tokens,), 0.01, device="cuda")
+    alone = [call(torch, *a, dloss) for a in args]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    need = cgx.cgx_head_distill_workspace(tokens, width, vocab, entries, cgx.BF16, True)
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    out = [{k: torch.empty_like(v) for k, v in a.items()} for a in alone]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for a, o, w, s in zip(args, out, ws, streams):
+            cgx.cgx_head_distill(*a, o["loss"], o["lse"], o["picked"], w, stream=s)
+            cgx.cgx_head_distill_grad(*a, o["lse"], o["picked"], dloss, o["dhidden"], o["dweight"], w, stream=s)
+    torch.cuda.synchronize()
+    for a, o in zip(alone, out):
+        assert all(torch.equal(a[k], o[k]) for k in a)

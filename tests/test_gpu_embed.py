@@ -354,3 +354,16 @@ def test_the_longest_vocabulary(torch, tokens):
     out = torch.empty(tokens, 1, dtype=torch.bfloat16, device="cuda")
     cgx.cgx_embed(dtable, ids, out)
     assert out[:, 0].tolist() == [want[k] for k in ids.tolist()]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [3, 300])
+def test_the_widest_rows(torch, tokens, dtype):
+    g = torch.Generator().manual_seed(tokens)
+    width, vocab = 1 << 17, 6
+    ids = torch.randint(0, vocab, (tokens,), generator=g).cuda()
+    table = torch.randn(vocab, width, generator=g).to(dtype_of(torch, dtype)).cuda()
+    look_up(torch, table, ids, scale=0.5)
+    dout = torch.randn(tokens, width, generator=g).to(table.dtype).cuda()
+    gradient(torch, dout, ids, vocab)
+    gradient(torch, dout, ids, vocab, before=table)

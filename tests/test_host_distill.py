@@ -42,9 +42,9 @@ def test_types_and_temperatures_that_are_refused(lib):
     for call in (loss, grad):
         for dt in (3, -1, 1 << 20):
             assert call(lib, teacher=dt) == DTYPE
-        for t in (0.0, -1.0, float("nan"), float("inf"), 2.0**-65, 2.0**65):
+        for t in (0.0, -1.0, float("nan"), float("inf"), 2.0**-10 * (1 - 2.0**-24), 2.0**10 * (1 + 2.0**-23), 2.0**-64, 2.0**64):
             assert call(lib, temperature=t) == SIZE
-        for t in (2.0**-64, 2.0**64):                             # (these pass: the workspace is what is refused)
+        for t in (2.0**-10, 2.0**10):                             # (these pass: the workspace is what is refused)
             assert call(lib, temperature=t, size=16) == SIZE and call(lib, (None,) * 10 if call is grad else (None,) * 8, temperature=t) == NULL
 
 
