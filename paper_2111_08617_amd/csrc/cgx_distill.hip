@@ -190,6 +190,12 @@ __global__ __launch_bounds__(64 * kFewRowWaves) void few_rows(Teacher teacher, i
             copy_row(weight.src + row * weight.width, weight.width, weight.dst + row * weight.pitch, weight.pitch, lane, 64);
         return;
     }
+    // (the other waves copy the row meanwhile, and take it back if it turns out to have no part)
+    const auto copy = [&](const T *source) {
+        copy_row(source, width, rows + token * pitch, pitch, tid - 64, 64 * (kFewRowWaves - 1));
+        if (LOWER) copy_row(source, width, rows + (lower + token) * pitch, pitch, tid - 64, 64 * (kFewRowWaves - 1));
+    };
+    if (wave > 0) copy(token < tokens ? hidden + token * width : nullptr);
     if (wave == 0) {
         TeacherRow r{0.f, 0.f, false};
         if (token < tokens) r = row_entries<M, true>(teacher, token, lane, s, entries, shares, nullptr, 0);
@@ -217,9 +223,7 @@ __global__ __launch_bounds__(64 * kFewRowWaves) void few_rows(Teacher teacher, i
         }
     }
     __syncthreads();
-    const T *const source = takes_part ? hidden + token * width : nullptr;
-    copy_row(source, width, rows + token * pitch, pitch, tid, 64 * kFewRowWaves);
-    if (LOWER) copy_row(source, width, rows + (lower + token) * pitch, pitch, tid, 64 * kFewRowWaves);
+    if (wave > 0 && token < tokens && !takes_part) copy(nullptr);
 }
 
 // A sum over the lanes of WAVES waves, in a fixed order; in the first of them.
@@ -302,6 +306,50 @@ template <typename T, bool LOWER>
 __global__ __launch_bounds__(256) void delta_entries(const Header *header, Entries entries, T *__restrict__ delta)
 {
     put_entry<T, T, LOWER>(entries, int64_t(blockIdx.x) * 256 + threadIdx.x, header, delta);
+}
+
+// d of few logits, entries and all: a block per 16 tokens and kFewColumns columns, whose waves sum a quarter of the width each (few_tiles), where tiles would
+// leave most of the chip idle and sum all of it.  125 x 519 x 1003 binary32: 6.8 us, tiles and their entries 13.3 and 4.  Rows and columns behind the
+// last ones are zeros, up to whole tiles and steps of the products.
+constexpr int kFewEntries = 256;                     // a token, at most: every block looks at all of its tokens'
+template <typename T, bool LOWER>
+__global__ __launch_bounds__(64 * kFewWaves, 4) void few_delta(const T *__restrict__ hidden, const T *__restrict__ weight, int64_t width, int64_t tokens,
+                                                               uint32_t groups, Entries entries, T *__restrict__ delta)
+{
+    __shared__ __align__(16) float part[kFewWaves][16][kFewPitch];
+    __shared__ float share[16][kFewColumns];
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t n0 = int64_t(blockIdx.x / groups) * kFewColumns, m0 = int64_t(blockIdx.x % groups) * 16;
+    const int64_t columns = entries.columns - n0, count = tokens - m0;
+    constexpr int kEach = 16 * kFewColumns / (64 * kFewWaves), kLanes = kFewColumns / kEach;
+    const int m = tid / kLanes, first = tid % kLanes * kEach;
+    const int64_t token = m0 + m;
+    const float base = m < count ? entries.lse[token] : 0.f, f = m < count ? entries.factor[token] : 0.f;
+    for (int k = tid; k < 16 * kFewColumns; k += 64 * kFewWaves) share[k / kFewColumns][k % kFewColumns] = 0.f;
+    __syncthreads();
+    if (f != 0.f)                                        // (others may have no sorted entries)
+        for (int k = tid % kLanes; k < entries.count; k += kLanes) {
+            const int64_t at = token * entries.count + k, column = int64_t(entries.entries[at].id) - entries.from - n0;
+            const float q = entries.shares[at];
+            if (entries.entries[at].id >= 0 && column >= 0 && column < kFewColumns) share[m][column] = q;
+        }
+    if (columns > 0 && count > 0)
+        few_products(part, hidden + m0 * width, weight + n0 * width, width, int(columns < kFewColumns ? columns : kFewColumns), int(count < 16 ? count : 16), wave, lane);
+    __syncthreads();
+    typedef T Vec __attribute__((ext_vector_type(kEach)));
+    Vec upper, rest;
+#pragma unroll
+    for (int e = 0; e < kEach; e++) {
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; k++) z += part[k][m][first + e];
+        const float d = f == 0.f || first + e >= columns ? 0.f : (lifted<T>(z * entries.inverse, base) - share[m][first + e] * float(1 << lift_of<T>)) * f;
+        upper[e] = T(d);
+        rest[e] = T(d - float(upper[e]));
+    }
+    T *const out = delta + token * entries.piece + n0 + first;
+    *reinterpret_cast<Vec *>(out) = upper;
+    if (LOWER) *reinterpret_cast<Vec *>(out + lower_rows(tokens) * entries.piece) = rest;
 }
 
 // bfloat16 to binary16, whose smaller range takes what is multiplied by a power of two, exactly: one that brings the largest magnitude into [2^14, 2^15).
@@ -458,6 +506,7 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
     const int64_t all = l.head.tokens * l.entries;
     const bool few = l.head.tokens > 0 && l.head.tokens <= kLowerTokens;
     calls.copied = few;
+    calls.few_logits = few && !l.other && calls.few_of_both() && l.entries <= kFewEntries;
     const auto prepare_few = [&](auto most) {
         constexpr int M = decltype(most)::value;
         const int64_t columns = l.head.padded ? l.head.columns(0) : 0, wanted = (columns + kFewRowWaves - 1) / kFewRowWaves;
@@ -491,6 +540,12 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
             convert_rows<false><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
             calls.launched();
             convert_rows<true><<<dim3(kConvertBlocks + blocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
+            calls.launched();
+        } else if (calls.few_logits) {
+            const uint32_t groups = uint32_t(lower_rows(l.head.tokens) / 16), wide = uint32_t((columns + 63) / 64 * 64 / kFewColumns);
+            few_delta<T, sizeof(T) == 2><<<dim3(groups * wide), 64 * kFewWaves, 0, stream>>>(
+                static_cast<const T *>(b.hidden), static_cast<const T *>(b.weight) + first * l.head.width, l.head.width, l.head.tokens, groups, n,
+                calls.template at<T>(l.head.delta));
             calls.launched();
         } else {
             if (l.lower) delta_entries<T, sizeof(T) == 2><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));

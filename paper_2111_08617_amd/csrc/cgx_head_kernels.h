@@ -513,33 +513,17 @@ __device__ __forceinline__ void entry_dots(const T *x, const T *weight, int64_t 
 // 16 x 768 x 30522 binary32 28 and 38; 103 MB that the memory-side cache partly holds 23 and 22, that it does not 25 and 27.  For 32 and 64
 // tokens the same with two and four times the tokens per wave was slower than the tiles (206 MB 62 and 62, 84 and 62): tokens then cost as
 // many bytes of the caches as W or more.  32 columns a block: 16 and 64 took 59 and 51 instead of 49 for 16 x 2048 x 50257.
-constexpr int kFewWaves = 4;
-template <typename T, typename S>
-__global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, const T *__restrict__ hidden, const T *__restrict__ weight,
-                                                               int64_t width, uint32_t groups, int64_t parts, float2 *__restrict__ stats,
-                                                               float *__restrict__ picked, S softmax, typename S::Picks picks)
+constexpr int kFewWaves = 4, kFewPitch = kFewColumns + 4;
+// What a wave's quarter of the width adds to the logits of `count` rows of hidden states (at most 16 are looked at) and `columns` of the weight.
+template <typename T>
+__device__ __forceinline__ void few_products(float (&part)[kFewWaves][16][kFewPitch], const T *__restrict__ hidden, const T *__restrict__ weight, int64_t width,
+                                             int columns, int count, int wave, int lane)
 {
     using E = Element<T>;
     using Frag = typename E::Frag;
     typedef Frag Anywhere __attribute__((aligned(sizeof(T))));         // (rows start at any element)
-    constexpr int TN = kFewColumns / 16, kUnit = kStepBytes / int(sizeof(T)), kPitch = kFewColumns + 4;
-    __shared__ __align__(16) float part[kFewWaves][16][kPitch];
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
-    uint32_t at_block = blockIdx.x;
-    if constexpr (!S::kTargets) {
-        if (at_block < picks.blocks) {                   // (their products take a few dependent loads, so they go ahead of W)
-            const int64_t item = int64_t(at_block) * kFewWaves + wave, each = (picks.count + kDots - 1) / kDots, token = item / each;
-            if (token >= tokens.tokens) return;
-            float *const out = picks.picked + token * picks.count;
-            entry_dots(hidden + token * width, weight, width, tokens.vocab, picks.ids + token * picks.count, picks.ignore, int(item % each) * kDots,
-                       picks.count, lane, [&](int k, int64_t, bool, float z) { if (lane == 0) out[k] = z; });
-            return;
-        }
-        at_block -= picks.blocks;
-    }
-    const uint32_t block = at_block / groups;
-    const int64_t n0 = int64_t(block) * kFewColumns, m0 = int64_t(at_block % groups) * kFewTokens;
-    const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens - m0);
+    constexpr int TN = kFewColumns / 16, kUnit = kStepBytes / int(sizeof(T));
+    const int g = lane >> 4, r = lane & 15;
     // (rows past the last one are read from it, and not used)
     uint32_t of_column[TN];
     const uint32_t of_token = uint32_t(r < count ? r : count - 1) * uint32_t(width * sizeof(T)) + g * 16;
@@ -549,7 +533,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
         Frag a[2], b[2][TN];
     };
     const int units = int(width / kUnit), from = units * wave / kFewWaves, to = units * (wave + 1) / kFewWaves;
-    const unsigned char *w = reinterpret_cast<const unsigned char *>(weight + n0 * width), *x = reinterpret_cast<const unsigned char *>(hidden + m0 * width);
+    const unsigned char *w = reinterpret_cast<const unsigned char *>(weight), *x = reinterpret_cast<const unsigned char *>(hidden);
     const auto load = [&](Unit &u, int at) {
 #pragma unroll
         for (int half = 0; half < 2; half++)
@@ -607,6 +591,31 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, co
     }
 #pragma unroll
     for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(&part[wave][r][16 * j + 4 * g]) = acc[j];
+}
+
+template <typename T, typename S>
+__global__ __launch_bounds__(64 * kFewWaves, 4) void few_tiles(Tokens tokens, const T *__restrict__ hidden, const T *__restrict__ weight,
+                                                               int64_t width, uint32_t groups, int64_t parts, float2 *__restrict__ stats,
+                                                               float *__restrict__ picked, S softmax, typename S::Picks picks)
+{
+    __shared__ __align__(16) float part[kFewWaves][16][kFewPitch];
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint32_t at_block = blockIdx.x;
+    if constexpr (!S::kTargets) {
+        if (at_block < picks.blocks) {                   // (their products take a few dependent loads, so they go ahead of W)
+            const int64_t item = int64_t(at_block) * kFewWaves + wave, each = (picks.count + kDots - 1) / kDots, token = item / each;
+            if (token >= tokens.tokens) return;
+            float *const out = picks.picked + token * picks.count;
+            entry_dots(hidden + token * width, weight, width, tokens.vocab, picks.ids + token * picks.count, picks.ignore, int(item % each) * kDots,
+                       picks.count, lane, [&](int k, int64_t, bool, float z) { if (lane == 0) out[k] = z; });
+            return;
+        }
+        at_block -= picks.blocks;
+    }
+    const uint32_t block = at_block / groups;
+    const int64_t n0 = int64_t(block) * kFewColumns, m0 = int64_t(at_block % groups) * kFewTokens;
+    const int columns = int(tokens.vocab - n0 < kFewColumns ? tokens.vocab - n0 : kFewColumns), count = int(tokens.tokens - m0);
+    few_products(part, hidden + m0 * width, weight + n0 * width, width, columns, count, wave, lane);
     __syncthreads();
     // a token's columns: kLanes neighbouring lanes, kEach columns a lane
     constexpr int kEach = 16 * kFewColumns / (64 * kFewWaves), kLanes = kFewColumns / kEach;
@@ -1042,6 +1051,7 @@ struct Calls {
     typename S::Picks picks = typename S::Picks();
     int32_t *tokens_of_rows = nullptr;
     bool lower = false;
+    bool few_logits = false;                                               // d is formed by what entries() queues
     bool copied = false;                                                   // hidden states are read from their copies, whichever tokens count
     D *hidden_of_products = nullptr, *weight_of_products = nullptr;        // where D is another type
     float *scales = nullptr;                                               // of the hidden states, of the weight's piece: 1 / the power of two
@@ -1132,8 +1142,10 @@ struct Calls {
     {
         const bool words = l.width * sizeof(T) % 4 == 0;
         const bool twice = l.padded && words && l.vocab < int64_t(1) << 27;      // (two groups' grid stays under 2^32 threads)
-        return l.tokens <= (twice ? 2 * kFewTokens : kFewTokens) || (words && tiles(l.tokens, l.vocab, 64) <= kFewTiles);
+        return l.tokens <= (twice ? 2 * kFewTokens : kFewTokens) || few_of_both();
     }
+    // (what few() says of few logits)
+    bool few_of_both() const { return l.width * sizeof(T) % 4 == 0 && tiles(l.tokens, l.vocab, 64) <= kFewTiles; }
     bool direct() const { return few() || (l.tokens <= kDirectTokens && !l.padded); }
     Tokens tokens() const
     {
@@ -1254,7 +1266,8 @@ struct Calls {
             const T *w = l.tokens ? weight(first, columns) : nullptr;
             if (l.tokens) {
                 const Size size = lower ? kTiny : size_of<T>(l.tokens, columns);
-                if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                if (few_logits) {
+                } else if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns);
                 entries(w, first, columns);
