@@ -355,7 +355,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_delta(const T *__restri
 // bfloat16 to binary16, whose smaller range takes what is multiplied by a power of two, exactly: one that brings the largest magnitude into [2^14, 2^15).
 // Then everything down to 2^-31 of the largest keeps its eight bits.  The first pass converts with a guess of that power, and remembers the largest
 // magnitude its blocks saw; the second one converts again only where that did not come into [2^3, 2^15): down to 2^-20 of the largest all bits are kept then.
-// Bound by memory: 30522 x 768 weights 16 us, 50257 x 2048 and 8192 x 2048 hidden states in two pieces 97; the second pass 5 us where it finds nothing to do.
+// Bound by memory: in launches of its own the first pass took 16 us for 30522 x 768 weights, 97 for 50257 x 2048 and 8192 x 2048 hidden states in two pieces; as
+// the last blocks of d's launch 8, where d's tiles fill 1.4 rounds, and still 80 to 88, where they fill twelve and both want the same memory.  The second
+// pass takes 5 us where it finds nothing to do.
 struct Conversion {
     _Float16 *to;
     int64_t pieces;          // of 16 bytes, at most
@@ -366,59 +368,74 @@ constexpr int kHiddenGuess = 4, kWeightGuess = 10;   // largest hidden states of
 __device__ __forceinline__ float finite_magnitude(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
 __device__ __forceinline__ float block_most(float v)
 {
-    __shared__ float waves[4];
+    __shared__ float waves[8];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    for (uint32_t w = 0; w < blockDim.x / 64; w++) v = fmaxf(v, waves[w]);
     __syncthreads();
     return v;
 }
-// rows.to may be null: the hidden states are converted with the first piece of the weight.  The second pass' blocks behind the first kConvertBlocks see to
-// the teacher's entries.
 template <bool AGAIN>
-__global__ __launch_bounds__(256) void convert_rows(const Header *header, Hidden<__bf16> hidden, int64_t pitch, const __bf16 *__restrict__ source_weight,
-                                                    Conversion rows, Conversion weight, Entries entries, _Float16 *__restrict__ delta)
+__device__ __forceinline__ void convert(const Conversion &c, const __bf16 *source, int64_t pieces, uint32_t block, uint32_t blocks)
 {
-    if (AGAIN && blockIdx.x >= kConvertBlocks) {
-        put_entry<__bf16, _Float16, false>(entries, int64_t(blockIdx.x - kConvertBlocks) * 256 + threadIdx.x, header, delta);
-        return;
-    }
     typedef __bf16 From __attribute__((ext_vector_type(8)));
     typedef _Float16 To __attribute__((ext_vector_type(8)));
-    const auto convert = [&](const Conversion &c, const __bf16 *source, int64_t pieces) {
-        int shift = c.guess;
-        if (AGAIN) {
-            float v = 0.f;
-            for (int k = int(threadIdx.x); k < kConvertBlocks; k += 256) v = fmaxf(v, c.most[k]);
-            v = block_most(v);
-            const bool again = v > 0.f && !(ilogbf(v) + shift >= 3 && ilogbf(v) + shift < 15);
-            if (again) shift = 14 - ilogbf(v);
-            if (blockIdx.x == 0 && threadIdx.x == 0) *c.scale = ldexpf(1.f, -shift);
-            if (!again) return;
-        }
-        float most = 0.f;
-        for (int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x; k < pieces; k += int64_t(kConvertBlocks) * 256) {
-            const From v = reinterpret_cast<const From *>(source)[k];
-            To out;
+    int shift = c.guess;
+    if (AGAIN) {
+        float v = 0.f;
+        for (int k = int(threadIdx.x); k < kConvertBlocks; k += int(blockDim.x)) v = fmaxf(v, c.most[k]);
+        v = block_most(v);
+        const bool again = v > 0.f && !(ilogbf(v) + shift >= 3 && ilogbf(v) + shift < 15);
+        if (again) shift = 14 - ilogbf(v);
+        if (block == 0 && threadIdx.x == 0) *c.scale = ldexpf(1.f, -shift);
+        if (!again) return;
+    }
+    float most = 0.f;
+    for (int64_t k = int64_t(block) * blockDim.x + threadIdx.x; k < pieces; k += int64_t(blocks) * blockDim.x) {
+        const From v = reinterpret_cast<const From *>(source)[k];
+        To out;
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float x = float(v[e]);
-                if (!AGAIN) most = fmaxf(most, finite_magnitude(x));
-                out[e] = _Float16(ldexpf(x, shift));
-            }
-            reinterpret_cast<To *>(c.to)[k] = out;
+        for (int e = 0; e < 8; e++) {
+            const float x = float(v[e]);
+            if (!AGAIN) most = fmaxf(most, finite_magnitude(x));
+            out[e] = _Float16(ldexpf(x, shift));
         }
-        if (AGAIN) return;
-        most = block_most(most);
-        if (threadIdx.x == 0) c.most[blockIdx.x] = most;
-    };
+        reinterpret_cast<To *>(c.to)[k] = out;
+    }
+    if (AGAIN) return;
+    most = block_most(most);
+    if (threadIdx.x == 0) c.most[block] = most;
+}
+// rows.to may be null: the hidden states are converted with the first piece of the weight.
+template <bool AGAIN>
+__device__ __forceinline__ void convert_both(const Conversion &rows, const Conversion &weight, uint32_t block, uint32_t blocks, const Header *header,
+                                             Hidden<__bf16> hidden, const __bf16 *source_weight, int64_t pitch)
+{
     if (rows.to) {
         const int64_t count = header->count;
-        convert(rows, hidden.of(count), lower_rows(count) * pitch / 8);
+        convert<AGAIN>(rows, hidden.of(count), lower_rows(count) * pitch / 8, block, blocks);
     }
-    convert(weight, source_weight, weight.pieces);
+    convert<AGAIN>(weight, source_weight, weight.pieces, block, blocks);
+}
+// The first pass is done by the last blocks of the launch that forms d.
+struct FirstPass {
+    static constexpr bool kAny = true;
+    uint32_t blocks;
+    Conversion rows, weight;
+    __device__ __forceinline__ void operator()(uint32_t block, const Header *header, Hidden<__bf16> hidden, const __bf16 *source_weight, int64_t pitch) const
+    {
+        convert_both<false>(rows, weight, block, blocks, header, hidden, source_weight, pitch);
+    }
+};
+// The second one; its blocks behind the first kAgainBlocks see to the teacher's entries.
+constexpr uint32_t kAgainBlocks = 1024;
+__global__ __launch_bounds__(256) void convert_again(const Header *header, Hidden<__bf16> hidden, int64_t pitch, const __bf16 *__restrict__ source_weight,
+                                                     Conversion rows, Conversion weight, Entries entries, _Float16 *__restrict__ delta)
+{
+    if (blockIdx.x < kAgainBlocks) convert_both<true>(rows, weight, blockIdx.x, kAgainBlocks, header, hidden, source_weight, pitch);
+    else put_entry<__bf16, _Float16, false>(entries, int64_t(blockIdx.x - kAgainBlocks) * 256 + threadIdx.x, header, delta);
 }
 
 Teacher teacher_of(const DistillLayout &l, const DistillBuffers &b)
@@ -528,18 +545,21 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
         else if (l.entries <= 256) prepare_few(std::integral_constant<int, 256>());
         else prepare_few(std::integral_constant<int, kMostEntries>());
     };
+    const auto beside = [&](int64_t first, int64_t columns) {
+        if constexpr (calls.kOther) {
+            float *const most = reinterpret_cast<float *>(at(l.most));
+            return FirstPass{kConvertBlocks, Conversion{first == 0 ? calls.hidden_of_products : nullptr, 0, most, calls.scales, kHiddenGuess},
+                             Conversion{calls.weight_of_products, columns * l.head.pitch / 8, most + kConvertBlocks, calls.scales + 1, kWeightGuess}};
+        } else return Nothing();
+    };
     const auto entries = [&](const T *w, int64_t first, int64_t columns) {
         const Entries n{calls.template at<Entry>(l.entry), calls.template at<float>(l.share), l.entries, all, calls.template at<int32_t>(l.head.place),
                         calls.template at<float>(l.head.lse), calls.template at<float>(l.head.factor), picked, inverse, first, columns, l.head.piece};
         const uint32_t blocks = uint32_t((all + 255) / 256);
         if constexpr (calls.kOther) {
-            float *const most = reinterpret_cast<float *>(at(l.most));
-            const Conversion rows{first == 0 ? calls.hidden_of_products : nullptr, 0, most, calls.scales, kHiddenGuess};
-            const Conversion weight{calls.weight_of_products, columns * l.head.pitch / 8, most + kConvertBlocks, calls.scales + 1, kWeightGuess};
-            D *const delta = calls.template at<D>(l.head.delta);
-            convert_rows<false><<<dim3(kConvertBlocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
-            calls.launched();
-            convert_rows<true><<<dim3(kConvertBlocks + blocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, rows, weight, n, delta);
+            const FirstPass done = beside(first, columns);
+            convert_again<<<dim3(kAgainBlocks + blocks), 256, 0, stream>>>(calls.header(), calls.hidden(), l.head.pitch, w, done.rows, done.weight, n,
+                                                                           calls.template at<D>(l.head.delta));
             calls.launched();
         } else if (calls.few_logits) {
             const uint32_t groups = uint32_t(lower_rows(l.head.tokens) / 16), wide = uint32_t((columns + 63) / 64 * 64 / kFewColumns);
@@ -553,7 +573,7 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
             calls.launched();
         }
     };
-    const hipError_t rest = calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), listed, entries);
+    const hipError_t rest = calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), listed, beside, entries);
     return error != hipSuccess ? error : rest;
 }
 

@@ -10,7 +10,8 @@ hipError_t gradient_of(const HeadLayout &l, const HeadBuffers &b, const float *l
                        hipStream_t stream)
 {
     const Calls<T> calls{l, b, stream};
-    return calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), [&] { calls.list(dloss, lse); }, [](const T *, int64_t, int64_t) {});
+    return calls.gradient(static_cast<T *>(dhidden), static_cast<T *>(dweight), [&] { calls.list(dloss, lse); }, [](int64_t, int64_t) { return Nothing(); },
+                          [](const T *, int64_t, int64_t) {});
 }
 
 }  // namespace

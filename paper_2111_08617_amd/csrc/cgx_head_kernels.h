@@ -714,6 +714,13 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tok
 // From the upper parts of d to the lower ones, in rows: whole tiles of 64, and whole steps of the products that sum over them.
 __host__ __device__ __forceinline__ int64_t lower_rows(int64_t count) { return (count + 63) / 64 * 64; }
 
+// What the last blocks of d's launch do besides tiles: nothing, or another kernel's work that the products after d need.  It fills the compute units that the
+// last round of tiles leaves idle.
+struct Nothing {
+    static constexpr bool kAny = false;
+    uint32_t blocks = 0;
+};
+
 // d of a tile of a piece: logits as above, then dloss (exp(z - lse) - [v = target]) in its units, in the operands' type.
 // Every element of the piece's whole tiles is written; those of no token or no column are zeros.
 // d is rounded to the operands' type once, because the products that follow read it from the matrix cores' operands: its relative error,
@@ -725,13 +732,22 @@ __host__ __device__ __forceinline__ int64_t lower_rows(int64_t count) { return (
 // 8192 tokens x 2048 x 25344 columns, bfloat16: 709 us = 1.20 PFLOP/s, with 0.41 GB written at the tiles' ends while no products run.
 //
 // D: the type that d is held in, where that is not the operands' (see Calls).  LOWER: what rounding takes from d is held as well, lower_rows(count) rows on.
-template <typename K, typename S, typename D, bool LOWER>
+// BESIDE: what the launch's last blocks do instead of tiles (see Nothing).
+template <typename K, typename S, typename D, bool LOWER, typename BESIDE>
 __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *header, Hidden<typename K::T> hidden, const typename K::T *weight,
                                                            int64_t pitch, int64_t first, int64_t columns,
                                                            const int32_t *__restrict__ target, const float *__restrict__ lse,
-                                                           const float *__restrict__ factor, D *__restrict__ delta, int64_t piece, S softmax)
+                                                           const float *__restrict__ factor, D *__restrict__ delta, int64_t piece, S softmax,
+                                                           BESIDE beside)
 {
     using T = typename K::T;
+    if constexpr (BESIDE::kAny) {
+        const uint32_t of_tiles = gridDim.x - beside.blocks;
+        if (blockIdx.x >= of_tiles) {
+            beside(blockIdx.x - of_tiles, header, hidden, weight, pitch);
+            return;
+        }
+    }
     __shared__ __align__(256) Lds<K> lds;
     const int64_t count = header->count, lower = lower_rows(count);
     int tm, tn;
@@ -1209,13 +1225,13 @@ struct Calls {
         return error;
     }
 
-    template <typename K>
-    void delta(const T *w, int64_t first, int64_t columns) const
+    template <typename K, typename BESIDE>
+    void delta(const T *w, int64_t first, int64_t columns, const BESIDE &beside) const
     {
         const auto go = [&](auto in_two) {
-            delta_tiles<K, S, D, decltype(in_two)::value><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM))), K::kThreads, 0, stream>>>(
+            delta_tiles<K, S, D, decltype(in_two)::value, BESIDE><<<dim3(uint32_t(tiles(l.tokens, columns, K::BM)) + beside.blocks), K::kThreads, 0, stream>>>(
                 header(), hidden(), w, l.pitch, first, columns, at<int32_t>(l.target), at<float>(l.lse), at<float>(l.factor), at<D>(l.delta),
-                l.piece, softmax);
+                l.piece, softmax, beside);
             launched();
         };
         if constexpr (!S::kTargets && !kOther && sizeof(T) == 2 && K::BM < 256) {
@@ -1297,8 +1313,9 @@ struct Calls {
     static constexpr int kTopBits = std::is_same<D, _Float16>::value ? 14 : std::is_same<D, __bf16>::value ? kLift : 0;
     // listed(): queues the list of tokens and what the products' hidden states need; entries(w, first, columns): what d of a piece lacks, and what the
     // products' weights need.
-    template <class Listed, class Entries>
-    hipError_t gradient(T *dhidden, T *dweight, Listed listed, Entries entries) const
+    // beside(first, columns): what d's launch does besides.
+    template <class Listed, class Beside, class Entries>
+    hipError_t gradient(T *dhidden, T *dweight, Listed listed, Beside beside, Entries entries) const
     {
         listed();
         const Size sums = sums_size();
@@ -1308,9 +1325,9 @@ struct Calls {
             if (l.tokens) {
                 const Size size = lower ? kTiny : size_of<T>(l.tokens, columns);
                 if (few_logits) {
-                } else if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns);
-                else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns);
+                } else if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns, beside(first, columns));
+                else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns, beside(first, columns));
+                else delta<Tiny<T, kSumContiguous, kSumStrips>>(w, first, columns, beside(first, columns));
                 entries(w, first, columns);
                 const D *of;
                 if constexpr (kOther) of = weight_of_products;
