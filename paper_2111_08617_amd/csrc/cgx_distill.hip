@@ -296,7 +296,7 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_picked(T
     const int64_t first = token * teacher.entries;
     const bool takes_part = row.takes_part();
     const float total = takes_part ? log_sum<WAVES>(stats + (place ? int64_t(place[token]) : token) * pitch, parts, lane) : 0.f;
-    const float log_mass = row.top + logf(row.sum);
+    const float log_mass = logf(row.sum);
     float sum = 0.f;
     for (int k = lane; k < teacher.entries; k += kLanes) {
         const int64_t id = teacher.ids[first + k];
@@ -304,7 +304,8 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_picked(T
         else if (id < 0 || id >= teacher.vocab) picked[first + k] = __builtin_nanf("");
         else {
             const float scaled = teacher.logit(first + k) * teacher.inverse, q = row.share(scaled);
-            if (q > 0.f) sum += q * (scaled - log_mass + total - picked[first + k] * teacher.inverse);
+            // (log q from differences: what a teacher's logits have in common, however large, takes no bits from it)
+            if (q > 0.f) sum += q * ((scaled - row.top - log_mass) + (total - picked[first + k] * teacher.inverse));
         }
     }
     sum = lanes_sum<WAVES>(sum, lane);
