@@ -268,6 +268,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_parts(const int64_t *__rest
 // ids by each of a block's waves; 23 us in parts, the longest share (a fifth of the tokens) in 17 of them.  Whole gradients of 256 columns looking at all
 // ids and in parts: 16384 tokens 30.5 and 36.0 us, 32768 41.9 and 37.4, 65536 65 and 45, alike for 259, 5000 and 50257 entries.
 // Zeros alone: 206 MB in 26 us into the memory-side cache, in some 40 past it.
+// (Without a limit of its registers: 41 to 59 of them, no scratch memory.  A build that was forced to spill some faulted, its cause is not known.)
 constexpr int kFillBytes = 64 << 10;                 // of the table, a block
 template <bool FILL, bool PARTS>
 __global__ __launch_bounds__(kSortThreads) void sort_tokens(const int64_t *__restrict__ ids, uint32_t tokens, int64_t ignore, int64_t vocab,

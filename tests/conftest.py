@@ -21,14 +21,15 @@ def oracle():
     return _oracle
 
 
-# Tests whose helpers fill workspaces and outputs on the current stream and then give a call another stream (`stream=`): without an order between the two a
-# fill could still run, or already run again, while the call's kernels use what it fills.
+# Tests whose helpers fill workspaces and outputs on the current stream and then give a call another stream (`stream=`):
+# without an order between the two a fill could still run, or already run again, while the call's kernels use what it fills.
 ON_OTHER_STREAMS = {("test_gpu_distill.py", "test_on_another_stream"), ("test_gpu_embed.py", "test_on_another_stream"),
                     ("test_gpu_head.py", "test_same_call_same_bits_and_other_streams"), ("test_gpu_grad.py", "test_streams_and_graphs")}
 
 
 def in_order(call, current_stream):
-    """`call`, whose work on a stream of its own comes after all that is queued on the current stream before it, and ahead of all that is queued behind it."""
+    """`call`, whose work on a stream of its own comes after all that is queued on the current stream before it, and ahead of
+    all that is queued behind it."""
     @functools.wraps(call)
     def ordered(*args, stream=None, **kwargs):
         if stream is None:
