@@ -449,8 +449,8 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  * and dhidden, dweight as above.  Everything that is said above of logits, d, sums, hidden, weight, loss, lse, dloss, dhidden, dweight, overlaps
  * and sizes holds here too, with these arguments instead of targets:
  *   ids       device, tokens x entries int64 (8-byte aligned), in any order.  An entry that is `ignore` is none: its logit is not looked at and its
- *             picked is 0.  Entries of one token with the same id count as their sum.  Any other id outside [0, vocab) makes that token's
- *             loss and gradients NaN, and its picked.
+ *             picked is 0.  Entries of one token may have the same id: the loss is the sum above, in which each has its own q[n][k] log q[n][k],
+ *             and d takes their q together.  Any other id outside [0, vocab) makes that token's loss and gradients NaN, and that entry's picked.
  *   teacher   device, tokens x entries elements of teacher_dt (CGX_F32, CGX_F16 or CGX_BF16), aligned like its elements.  -infinity is a share of 0;
  *             NaN and +infinity make that token's loss and gradients NaN.
  *   picked    device, tokens x entries floats (4-byte aligned)
