@@ -607,8 +607,12 @@ hipError_t gradient_of(const DistillLayout &l, const DistillBuffers &b, const fl
                 calls.template at<T>(l.head.delta));
             calls.launched();
         } else {
-            if (l.lower) delta_entries<T, sizeof(T) == 2><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));
-            else delta_entries<T, false><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));
+            const auto go = [&](auto in_two) {
+                delta_entries<T, decltype(in_two)::value><<<dim3(blocks), 256, 0, stream>>>(calls.header(), n, calls.template at<T>(l.head.delta));
+            };
+            if constexpr (calls.kFewOnly) go(std::true_type());
+            else if (l.lower) go(std::bool_constant<sizeof(T) == 2>());
+            else go(std::false_type());
             calls.launched();
         }
     };

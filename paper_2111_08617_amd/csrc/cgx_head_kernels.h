@@ -1102,6 +1102,7 @@ struct Calls {
     D *hidden_of_products = nullptr, *weight_of_products = nullptr;        // where D is another type
     float *scales = nullptr;                                               // of the hidden states, of the weight's piece: 1 / the power of two
     static constexpr bool kOther = !std::is_same<D, T>::value;
+    static constexpr bool kFewOnly = !S::kTargets && std::is_same<D, __bf16>::value;       // d of more tokens is held in binary16
     mutable hipError_t error = hipSuccess;      // of the first launch that was refused
 
     void launched() const
@@ -1234,10 +1235,10 @@ struct Calls {
                 l.piece, softmax, beside);
             launched();
         };
-        if constexpr (!S::kTargets && !kOther && sizeof(T) == 2 && K::BM < 256) {
-            if (lower) return go(std::true_type());
+        if constexpr (!S::kTargets && !kOther && sizeof(T) == 2 && K::BM == 64) {
+            if (kFewOnly || lower) return go(std::true_type());
         }
-        go(std::false_type());
+        if constexpr (!kFewOnly) go(std::false_type());
     }
     // What the products of d run over: the rows that count, or (lower) two sections of them.
     Header *products() const { return header() + (lower ? 1 : 0); }
@@ -1292,9 +1293,9 @@ struct Calls {
             launched();
         };
         if constexpr (!S::kTargets && !kOther && sizeof(T) == 2) {
-            if (lower) return go(std::true_type());
+            if (kFewOnly || lower) return go(std::true_type());
         }
-        go(std::false_type());
+        if constexpr (!kFewOnly) go(std::false_type());
     }
     template <typename K>
     void weight_rows(int64_t first, int64_t columns, T *dweight) const
@@ -1306,9 +1307,11 @@ struct Calls {
             at<float>(l.spare), scales);
         launched();
         if (!rest || 2 * rest > blocks<K> || (product_rows() + K::kDepth - 1) / K::kDepth < 2 * kLeastSteps) return;
-        weight_rest<K, T, kOther><<<dim3(uint32_t(rest * (K::BM / 16))), 256, 0, stream>>>(products(), columns, l.width, blocks<K>,
-                                                                                        dweight + first * l.width, at<float>(l.spare), scales);
-        launched();
+        if constexpr (!kFewOnly) {                       // (few steps are not split)
+            weight_rest<K, T, kOther><<<dim3(uint32_t(rest * (K::BM / 16))), 256, 0, stream>>>(products(), columns, l.width, blocks<K>,
+                                                                                            dweight + first * l.width, at<float>(l.spare), scales);
+            launched();
+        }
     }
     static constexpr int kTopBits = std::is_same<D, _Float16>::value ? 14 : std::is_same<D, __bf16>::value ? kLift : 0;
     // listed(): queues the list of tokens and what the products' hidden states need; entries(w, first, columns): what d of a piece lacks, and what the
@@ -1323,7 +1326,7 @@ struct Calls {
             const int64_t first = k * l.piece, columns = l.columns(k);
             const T *w = l.tokens ? weight(first, columns) : nullptr;
             if (l.tokens) {
-                const Size size = lower ? kTiny : size_of<T>(l.tokens, columns);
+                const Size size = kFewOnly || lower ? kTiny : size_of<T>(l.tokens, columns);
                 if (few_logits) {
                 } else if (size == kLarge) delta<Large<T, kSumContiguous, kSumStrips>>(w, first, columns, beside(first, columns));
                 else if (size == kSmall) delta<Small<T, kSumContiguous, kSumStrips>>(w, first, columns, beside(first, columns));
