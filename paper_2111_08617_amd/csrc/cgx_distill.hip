@@ -337,9 +337,12 @@ __device__ __forceinline__ void put_entry(const Entries &n, int64_t k, const Hea
     if (e.id < 0 || column < 0 || column >= n.columns) return;
     const float z = n.picked[token * n.count + e.place];
     const float d = (lifted<T>(z * n.inverse, n.lse[row]) - n.shares[k] * float(1 << lift_of<T>)) * n.factor[row];
-    const D upper = D(d);
-    delta[row * n.piece + column] = upper;
-    if (LOWER) delta[(row + lower_rows(header->count)) * n.piece + column] = D(d - float(upper));
+    D *const out = delta + row * n.piece + column;
+    if constexpr (LOWER) {
+        const TwoParts<D> parts(d);
+        *out = parts.upper;
+        out[lower_rows(header->count) * n.piece] = parts.rest;
+    } else *out = D(d);
 }
 template <typename T, bool LOWER>
 __global__ __launch_bounds__(256) void delta_entries(const Header *header, Entries entries, T *__restrict__ delta)
@@ -383,8 +386,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_delta(const T *__restri
 #pragma unroll
         for (int k = 0; k < kFewWaves; k++) z += part[k][m][first + e];
         const float d = f == 0.f || first + e >= columns ? 0.f : (lifted<T>(z * entries.inverse, base) - share[m][first + e] * float(1 << lift_of<T>)) * f;
-        upper[e] = T(d);
-        rest[e] = T(d - float(upper[e]));
+        if constexpr (LOWER) {
+            const TwoParts<T> parts(d);
+            upper[e] = parts.upper;
+            rest[e] = parts.rest;
+        } else upper[e] = T(d);
     }
     T *const out = delta + token * entries.piece + n0 + first;
     *reinterpret_cast<Vec *>(out) = upper;

@@ -714,6 +714,20 @@ __global__ __launch_bounds__(64 * WAVES * join_tokens<WAVES>) void join_loss(Tok
 // From the upper parts of d to the lower ones, in rows: whole tiles of 64, and whole steps of the products that sum over them.
 __host__ __device__ __forceinline__ int64_t lower_rows(int64_t count) { return (count + 63) / 64 * 64; }
 
+// d in two parts of fewer bits.  The compiler may round a product to binary16 in one step for one use of it, and by way of binary32 for another:
+// where that makes a difference (one element in some ten thousand) the parts would be those of two numbers, a step of the upper one apart.
+// So d is a number in a register first.
+template <typename D>
+struct TwoParts {
+    D upper, rest;
+    explicit __device__ __forceinline__ TwoParts(float d)
+    {
+        asm("" : "+v"(d));
+        upper = D(d);
+        rest = D(d - float(upper));
+    }
+};
+
 // What the last blocks of d's launch do besides tiles: nothing, or another kernel's work that the products after d need.  It fills the compute units that the
 // last round of tiles leaves idle.
 struct Nothing {
@@ -780,8 +794,11 @@ __global__ __launch_bounds__(K::kThreads, 2) void delta_tiles(const Header *head
 #pragma unroll
             for (int e = 0; e < kPer; e++) {
                 const float d = lifted<T>(softmax.of(tile.acc[i][(k + e) / 4][(k + e) % 4]), base) * f;
-                v[e] = D(d);
-                if (LOWER) rest[e] = D(d - float(v[e]));
+                if constexpr (LOWER) {
+                    const TwoParts<D> parts(d);
+                    v[e] = parts.upper;
+                    rest[e] = parts.rest;
+                } else v[e] = D(d);
             }
             if (!whole || (!S::kTargets && !counts))
 #pragma unroll
