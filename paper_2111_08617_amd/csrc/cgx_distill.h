@@ -26,11 +26,13 @@ struct DistillLayout {
     size_t bytes = 0;
 };
 
-// us of the call with gradients with 128, 256, 512 and 1024 blocks: 615 of 4096 x 768 x 30522 228, 230, 233 and 236 (242 with a launch of its own),
-// 8192 x 2048 x 50257 5495, 5487, 5488 and 5474 (5496).
+// us of the call with gradients with 128, 256, 512 and 1024 blocks, the same inputs again and again: 615 of 4096 x 768 x 30522 228, 230, 233
+// and 236 (242 with a launch of its own), 8192 x 2048 x 50257 5495, 5487, 5488 and 5474 (5496).  (With other inputs from pass to pass the calls
+// with 256 take 250 and 5640.)
 constexpr int kConvertBlocks = 256;
-// Up to this many tokens of a gradient are not listed, and hold a 16-bit d in two parts: rows for both are there.  us with two parts and, for bfloat16 in
-// binary16, for binary16 in one: 128 x 2048 x 50257 326 and 403, 330 and 326; 256 x 2048 x 50257 458 and 438, 465 and 340.
+// Up to this many tokens of a gradient are not listed, and hold a 16-bit d in two parts: rows for both are there.  us of loss and gradients (the
+// same inputs again and again) with two parts and, for bfloat16 in binary16, for binary16 in one: 128 x 2048 x 50257 326 and 403, 330 and 326;
+// 256 x 2048 x 50257 458 and 438, 465 and 340.
 constexpr int64_t kLowerTokens = 128;
 
 // CGX_OK and the layout, or the error of the sizes.

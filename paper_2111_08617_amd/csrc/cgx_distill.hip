@@ -350,10 +350,15 @@ __global__ __launch_bounds__(256) void delta_entries(const Header *header, Entri
     put_entry<T, T, LOWER>(entries, int64_t(blockIdx.x) * 256 + threadIdx.x, header, delta);
 }
 
-// d of few logits, entries and all: a block per 16 tokens and kFewColumns columns, whose waves sum a quarter of the width each (few_tiles), where tiles would
-// leave most of the chip idle and sum all of it.  125 x 519 x 1003 binary32: 6.8 us, tiles and their entries 13.3 and 4.  Rows and columns behind the
-// last ones are zeros, up to whole tiles and steps of the products.
-constexpr int kFewEntries = 256;                     // a token, at most: every block looks at all of its tokens'
+// d of few logits, entries and all: a block per 16 tokens and kFewColumns columns, whose waves sum a quarter of the width each (few_tiles), where
+// tiles would leave most of the chip idle and sum all of it.  125 x 519 x 1003 binary32: 6.4 to 6.8 us, tiles and their entries 13.3 and 4.  Rows and
+// columns behind the last ones are zeros, up to whole tiles and steps of the products.
+// Taken for up to kFewTiles (64) tiles of logits.  us of whole gradients with it and with tiles: 128 x 512, 64 entries, 1000 columns (32 tiles)
+// binary32 24.4 and 31.1, bfloat16 23.1 and 26.3, binary16 22.6 and 26.0; 2000 (64) 29.8 and 33.1, 25.1 and 27.2, 25.1 and 27.1; 4000 (126) 38.7 and
+// 38.0, 30.4 and 28.9, 30.2 and 28.9; 8000 62 and 50, 44 and 36, 44 and 36; 16 x 512 x 4000 (63) 28.9 and 32.2, 23.1 and 24.6, 22.9 and 24.7.
+// Entries a token, at most: every block looks at all of its tokens'.  128 x 512 x 1000, 256 of them: 36.7 and 39.1, 33.7 and 32.5, 33.4 and 32.4;
+// 512: 76 and 74, 73 and 67, 73 and 67.
+constexpr int kFewEntries = 256;
 template <typename T, bool LOWER>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void few_delta(const T *__restrict__ hidden, const T *__restrict__ weight, int64_t width, int64_t tokens,
                                                                uint32_t groups, Entries entries, T *__restrict__ delta)

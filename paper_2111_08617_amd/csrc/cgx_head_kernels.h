@@ -993,8 +993,11 @@ __global__ __launch_bounds__(K::kThreads, 2) void weight_tiles(const Header *hea
     weight_block<K, OUT, SCALED>(lds, blockIdx.x, header, delta, piece, hidden, pitch, columns, width, blocks, dweight, spare, scale);
 }
 
-// Both products of d in one launch, where both take small tiles and neither fills the chip: a launch's time less (125 x 519 x 1003 binary32 9.8 us instead of 8.4 and 5.9
-// one after the other, and what lies between launches).
+// Both products of d in one launch, where both take small tiles and neither fills the chip: a launch's time less (125 x 519 x 1003 binary32
+// 8.9 us instead of 8.4 and 5.9 one after the other, and what lies between launches).  us of whole gradients in two launches and in one: 128 x
+// 512 x 1000 (128 tiles of the weight) binary32 28.6 and 23.5, bfloat16 27.4 and 22.6, binary16 27.3 and 22.7; 128 x 2048 x 2000 (1024, as many
+// as blocks fit the chip: the limit) 62.4 and 60.9, 44.6 and 42.3, 44.7 and 42.4; x 4000 (2016) 94.7 and 90.2, 60.6 and 55.3, 62.5 and 55.9;
+// x 8000 (4000) 128 and 124, alike in 16 bits, whose large tiles catch up there.
 template <typename KH, typename KW>
 __global__ __launch_bounds__(KH::kThreads, 2) void both_tiles(uint32_t of_hidden, const Header *header, const typename KH::T *delta, int64_t piece,
                                                            const typename KH::T *weight, int64_t pitch, int64_t columns, int32_t blocks,
