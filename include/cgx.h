@@ -456,9 +456,10 @@ int cgx_head_loss_grad(const void *hidden, const void *weight, const int64_t *ta
  *   picked    device, tokens x entries floats (4-byte aligned)
  * A token without an entry, or whose entries all have a share of 0, takes no part: loss, lse and picked 0, a dhidden row of zeros, nothing in
  * dweight, whatever its hidden state holds; so does, in cgx_head_distill_grad, one whose dloss is 0.
- * d is held more exactly here, since the entries' elements are not near 1 as a target's is: in two parts for up to 128 tokens, and in binary16 for
- * more tokens of bfloat16, whose operands then are converted as well: an element of d below 2^-28 of the largest dloss loses bits, one below 2^-39 is
- * lost, and so are bits of operands below 2^-20 of the largest one.
+ * d is held more exactly here, since the entries' elements are not near 1 as a target's is: in two parts for up to 128 tokens,
+ * and in binary16 for more tokens of bfloat16, whose operands then are converted as well.  In binary16 an element of d below
+ * 2^-28 of the largest dloss of a token that takes part loses bits, one below 2^-39 is lost; where bfloat16 operands are
+ * converted, so are bits of those below 2^-20 of the largest one.
  * 1 <= entries <= 1024 (more than vocab are allowed), tokens x entries < 2^31, 2^-10 <= temperature <= 2^10 (CGX_ERR_SIZE otherwise).
  * Logits over the temperature are formed in binary32, and a probability is off by some 2^-22 of the token's |lse|, as it is above.
  */
